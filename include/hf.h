@@ -562,6 +562,106 @@ HF_API int hf_rope_append_keys(const hf_config* cfg, const void* K_new, int32_t 
                         const float* rope_cos, const float* rope_sin,
                         void* K_win, int32_t first, int32_t n_kv, void* pooled_K, void* stream);
 
+/* ---- Rotation by positions with several axes -------------------------------------------------------
+ * hf_rope_tables covers the tokens of one grid in order; here every token carries its own positions, on the device: text in one
+ * axis, images and video in two or three (time, row, column), sequences of different lengths in one call. */
+#define HF_ROPE_MAX_AXES 4
+
+enum { HF_ROPE_ADJACENT = 0, HF_ROPE_HALVES = 1 };   /* hf_rope_axes.layout */
+enum { HF_ROPE_PER_AXIS = 0, HF_ROPE_SHARED = 1 };   /* hf_rope_axes.spectrum */
+
+/* Of a row of head_dim features the first 2 P turn, P = the sum of pairs[], the others stay as they are.  The first pairs[0] pairs
+ * turn by the first axis' position, the next pairs[1] by the second's, and so on. */
+typedef struct hf_rope_axes {
+  double  theta;       /* >= 1, finite */
+  int32_t n_axes;      /* 1 .. HF_ROPE_MAX_AXES */
+  int32_t pairs[HF_ROPE_MAX_AXES];   /* each >= 1 for the first n_axes, their sum P <= head_dim / 2 */
+  int32_t layout;      /* HF_ROPE_ADJACENT: pair p is the features (2p, 2p+1); HF_ROPE_HALVES: (p, p + P) */
+  int32_t spectrum;    /* radians per position step: HF_ROPE_PER_AXIS theta^(-i / pairs[a]) for pair i of axis a (as hf_rope_tables);
+                          HF_ROPE_SHARED theta^(-p / P) for pair p of all */
+} hf_rope_axes;
+
+/* Y = X with every pair turned by its angle, the token's position on the pair's axis times the pair's rate:
+ *     y[a] = x[a] cos - x[b] sin,   y[b] = x[a] sin + x[b] cos   for the pair's features (a, b)
+ * inverse != 0 turns the other way: the gradient with respect to X of the forward call, from the gradient with respect to Y.
+ *   dtype, head_dim  HF_BF16 | HF_F32, 64 or 128
+ *   X, Y       [batch, heads, n_tokens, head_dim], head_dim innermost and contiguous; x_strides, y_strides: HOST int64 [3], distances
+ *              between batches, heads and tokens in elements, multiples of 16 bytes; NULL: contiguous.  An X stride may be zero.
+ *              Rows of Y may not overlap (each stride covers what the smaller ones span).  Y may be X (the same address and strides);
+ *              otherwise the two address ranges must be disjoint.
+ *   positions  device int32 [n_axes, n_tokens] for all batches, or, positions_per_batch != 0, [batch, n_axes, n_tokens]; any value
+ *   n_tokens   0 is allowed: nothing is enqueued
+ * Angles are reduced in 64 bits; sine, cosine and the products are fp32 (the first two off by 2.5 units of 2^-24 at most), with one rounding to dtype. */
+HF_API int hf_rope_axes_apply(const hf_rope_axes* rope, int32_t dtype, int32_t head_dim, int32_t batch, int32_t heads, int32_t n_tokens,
+                  const void* X, const int64_t* x_strides, const int32_t* positions, int32_t positions_per_batch,
+                  void* Y, const int64_t* y_strides, int32_t inverse, void* stream);
+
+/* ---- A cache of pages that many sequences share --------------------------------------------------------
+ * The window calls above keep the keys and values of sequences of ONE length side by side.  Here a pool of pages of page_tokens tokens
+ * each holds sequences (prompts, streams) of any lengths; a table names the pages of every sequence in order.  A page may be a latent
+ * frame of a video stream, or some tens of text tokens.
+ *
+ *   K_pages, V_pages  [n_pages, heads_kv, page_tokens, head_dim] of dtype, contiguous
+ *   page_table  device int32 [n_seqs, max_pages]: tokens page_tokens * i .. of sequence s lie in page page_table[s][i].  An entry outside
+ *               [0, n_pages) is no page: what should be written there is dropped, what should be read from there is masked.  Sequences
+ *               may share pages that no call writes meanwhile (a common beginning).
+ *   cu_new      device int32 [n_seqs + 1], ascending from 0: the new tokens of sequence s are the rows cu_new[s] .. cu_new[s+1] - 1 of
+ *               the packed operands.  A sequence may have none.  Rows from cu_new[n_seqs] on are neither read into anything nor written.
+ *   seq_lens    device int32 [n_seqs]: tokens of every sequence, the new ones INCLUDED: new token i of a sequence with m of them and
+ *               length n is token n - m + i (its place).  Tokens at a negative place or behind max_pages * page_tokens do not exist.
+ * All lengths and tables are read on the device: a captured call follows what they hold when it is replayed.
+ *
+ * Packed operands are [rows, heads, head_dim] with head_dim contiguous; their strides arguments are HOST int64 [2], distances between
+ * rows and between heads in elements, multiples of 16 bytes (a view into the rows of a joint projection); NULL: contiguous. */
+typedef struct hf_paged {
+  int32_t heads;          /* query heads */
+  int32_t heads_kv;       /* key and value heads; query head h reads head h / (heads / heads_kv) */
+  int32_t head_dim;       /* 64 or 128 */
+  int32_t dtype;          /* HF_BF16 | HF_F32 */
+  int32_t page_tokens;    /* 1 .. 65536 */
+  int32_t n_pages;        /* pages of the pool, >= 1 */
+  int32_t n_seqs;         /* 1 .. 65535 */
+  int32_t max_pages;      /* entries of a table row, >= 1; max_pages * page_tokens <= 2^30 */
+  int32_t causal;         /* 0: a token sees every token of its sequence (a chunk of frames); else those up to its own place */
+  int32_t window;         /* 0: no limit; > 0: a token at place p sees the places behind p - window only, and */
+  int32_t n_sink;         /* the sequence's first n_sink tokens (without a window: no meaning) */
+  float   softmax_scale;  /* 0 means 1/sqrt(head_dim) */
+} hf_paged;
+
+/* New keys, rotated by their positions, and new values enter the pages; the queries of the same tokens are rotated in the same launch.
+ *   K_new, V_new  packed [n_new, heads_kv, head_dim]; Q, Q_out packed [n_new, heads, head_dim], both or neither; Q_out may be Q (same
+ *             address and strides), otherwise their address ranges must be disjoint, and Q_out's rows may not overlap each other.
+ *             K_new, V_new may interleave with Q_out (rows of one joint projection) but not share elements with it
+ *   rope      NULL: keys (and queries) are copied as they are
+ *   positions device int32 [n_axes, n_new]; NULL: a token's position on every axis is its place
+ * A key is written as hf_rope_axes_apply would write it.  Two tokens of one call that name the same slot (tables that share a page
+ * which is written to) leave either of them there, or parts of both.  n_new = 0 enqueues nothing. */
+HF_API int hf_paged_append(const hf_paged* cache, const hf_rope_axes* rope_or_null, int32_t n_new,
+                  const void* K_new, const int64_t* k_strides, const void* V_new, const int64_t* v_strides,
+                  const void* Q_or_null, const int64_t* q_strides, const int32_t* cu_new, const int32_t* seq_lens,
+                  const int32_t* positions, void* K_pages, void* V_pages, const int32_t* page_table,
+                  void* Q_out, const int64_t* q_out_strides, void* stream);
+
+/* Bytes of scratch hf_paged_attn_fwd needs for n_q packed rows, whatever the lengths are.  Host-only. */
+HF_API int hf_paged_workspace_bytes(const hf_paged* cache, int32_t n_q, size_t* bytes_out);
+
+/* Attention of every sequence's new tokens over its pages (their own keys and values have been appended before):
+ *     O = sum_j softmax_j(softmax_scale q . k_j) v_j   over the keys j that the token sees (causal, window, n_sink of the cache)
+ * One token a sequence (decoding), a few, or whole chunks; sequences of both kinds in one call.
+ *   Q, O      packed [n_q, heads, head_dim]; O must not overlap Q, and its rows may not overlap each other
+ *   lse2_or_null  out fp32 [heads, n_q]: log2 of the softmax denominator, logits scaled by softmax_scale * log2(e), as
+ *             hf_hybrid_attn_fwd_save writes it: parts of an attention over several caches can be joined by it
+ *   workspace >= hf_paged_workspace_bytes(cache, n_q) bytes, 256-byte aligned, no initialisation needed; two calls that may overlap in
+ *             time must not share one
+ * A token that sees no key gets O = 0 and lse2 = +inf.  What a token does not see, it does not depend on, a NaN or an infinity
+ * there included.  fp32 scores, statistics and sums; in bf16 the probabilities are rounded to bf16 for the second product.  The keys of
+ * a sequence may be shared out over workgroups by what the lengths of the whole batch leave idle, so that the rounding of a row's fp32
+ * sums depends on its batch; one batch gives the same bits every time.  n_q = 0 enqueues nothing. */
+HF_API int hf_paged_attn_fwd(const hf_paged* cache, const void* Q, const int64_t* q_strides, int32_t n_q,
+                  const int32_t* cu_new, const int32_t* seq_lens, const void* K_pages, const void* V_pages,
+                  const int32_t* page_table, void* O, const int64_t* o_strides, float* lse2_or_null,
+                  void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- Measurement helper (no part of the method) ------------------------------------------------ */
 
 /* Enqueues a kernel in which 2048 wavefronts (two per SIMD of a 256-unit chip) each issue iters * 16 independent

@@ -16,6 +16,9 @@ import torch
 HF_BF16, HF_F32 = 0, 1
 HF_PHI_RELU, HF_PHI_ELU1 = 0, 1
 HF_FLAG_READOUT_KERNEL, HF_FLAG_HISTORY_TWO_PLANES, HF_FLAG_BWD_FP32_KERNELS, HF_FLAG_DKV_INDEX_ORDER = 1, 2, 4, 8
+HF_ROPE_ADJACENT, HF_ROPE_HALVES = 0, 1
+HF_ROPE_PER_AXIS, HF_ROPE_SHARED = 0, 1
+HF_ROPE_MAX_AXES = 4
 HF_OK = 0
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libhf.so")
@@ -57,14 +60,43 @@ class hf_ring(ctypes.Structure):
                 ("next_slot", ctypes.c_int32), ("cur_slot", ctypes.c_int32), ("absorbed_ahead", ctypes.c_int32)]
 
 
+class hf_rope_axes(ctypes.Structure):
+    _fields_ = [("theta", ctypes.c_double), ("n_axes", ctypes.c_int32), ("pairs", ctypes.c_int32 * HF_ROPE_MAX_AXES),
+                ("layout", ctypes.c_int32), ("spectrum", ctypes.c_int32)]
+
+
+class hf_paged(ctypes.Structure):
+    _fields_ = [("heads", ctypes.c_int32), ("heads_kv", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("page_tokens", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("n_seqs", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("causal", ctypes.c_int32), ("window", ctypes.c_int32), ("n_sink", ctypes.c_int32), ("softmax_scale", ctypes.c_float)]
+
+
+def _dtype(dtype):
+    if isinstance(dtype, str):
+        return {"bf16": HF_BF16, "f32": HF_F32}[dtype]
+    if isinstance(dtype, torch.dtype):
+        return {torch.bfloat16: HF_BF16, torch.float32: HF_F32}[dtype]
+    return dtype
+
+
 def make_config(batch, heads, head_dim, dtype, block_q, block_kv, keep_ratio=1.0, keep_k=0,
                 phi=HF_PHI_RELU, eps=1e-6, z_scale=1.0, softmax_scale=0.0, kv_capacity=0, flags=0) -> hf_config:
-    if isinstance(dtype, str):
-        dtype = {"bf16": HF_BF16, "f32": HF_F32}[dtype]
-    elif isinstance(dtype, torch.dtype):
-        dtype = {torch.bfloat16: HF_BF16, torch.float32: HF_F32}[dtype]
-    return hf_config(batch, heads, head_dim, dtype, block_q, block_kv, keep_ratio, keep_k, phi, eps,
+    return hf_config(batch, heads, head_dim, _dtype(dtype), block_q, block_kv, keep_ratio, keep_k, phi, eps,
                      z_scale, softmax_scale, kv_capacity, flags)
+
+
+def make_rope_axes(pairs, theta=10000.0, layout=HF_ROPE_HALVES, spectrum=HF_ROPE_SHARED) -> hf_rope_axes:
+    """pairs: feature pairs of every axis; hf_rope_tables' convention is layout ADJACENT with spectrum PER_AXIS."""
+    pairs = list(pairs)
+    if len(pairs) > HF_ROPE_MAX_AXES:
+        raise ValueError(f"at most {HF_ROPE_MAX_AXES} axes")
+    return hf_rope_axes(theta, len(pairs), (ctypes.c_int32 * HF_ROPE_MAX_AXES)(*pairs), layout, spectrum)
+
+
+def make_paged(heads, heads_kv, head_dim, dtype, page_tokens, n_pages, n_seqs, max_pages, causal=True, window=0, n_sink=0,
+               softmax_scale=0.0) -> hf_paged:
+    return hf_paged(heads, heads_kv, head_dim, _dtype(dtype), page_tokens, n_pages, n_seqs, max_pages, int(causal), window, n_sink,
+                    softmax_scale)
 
 
 def lib_path() -> str:
@@ -125,6 +157,11 @@ def load():
     lib.hf_rope_tables.argtypes = [ctypes.POINTER(I), I, I, I, I, I, I, ctypes.c_double, I, P, P, P]
     lib.hf_rope_apply.argtypes = [CP, P, I, P, P, P, P]
     lib.hf_rope_append_keys.argtypes = [CP, P, I, P, P, P, I, I, P, P]
+    AP, PP, LP = ctypes.POINTER(hf_rope_axes), ctypes.POINTER(hf_paged), ctypes.POINTER(ctypes.c_int64)
+    lib.hf_rope_axes_apply.argtypes = [AP, I, I, I, I, I, P, LP, P, I, P, LP, I, P]
+    lib.hf_paged_append.argtypes = [PP, AP, I, P, LP, P, LP, P, LP, P, P, P, P, P, P, P, LP, P]
+    lib.hf_paged_workspace_bytes.argtypes = [PP, I, ctypes.POINTER(SZ)]
+    lib.hf_paged_attn_fwd.argtypes = [PP, P, LP, I, P, P, P, P, P, P, LP, P, P, SZ, P]
     lib.hf_probe_mfma_bf16.argtypes = [I, P, ctypes.POINTER(ctypes.c_double), P]
     for name in ("hf_state_bytes", "hf_state_init", "hf_state_fold_linear", "hf_window_advance", "hf_absorb_evicted", "hf_absorb_workspace_bytes", "hf_select_k",
                  "hf_workspace_bytes",
@@ -134,14 +171,15 @@ def load():
                  "hf_stream_step", "hf_bwd_workspace_bytes", "hf_bwd_least_workspace_bytes", "hf_hybrid_attn_bwd", "hf_state_planes_bytes",
                  "hf_state_planes", "hf_absorb_evicted_planes", "hf_hybrid_attn_fwd_planes", "hf_probe_mfma_bf16",
                  "hf_ring_open_chunk", "hf_ring_step", "hf_pooled_keys_bytes", "hf_pool_keys", "hf_select_attn_fwd",
-                 "hf_step_workspace_bytes", "hf_step_fwd", "hf_rope_append_keys", "hf_ring_last_step"):
+                 "hf_step_workspace_bytes", "hf_step_fwd", "hf_rope_append_keys", "hf_ring_last_step", "hf_rope_axes_apply", "hf_paged_append",
+                 "hf_paged_workspace_bytes", "hf_paged_attn_fwd"):
         getattr(lib, name).restype = ctypes.c_int
     try:
         from . import _marshal
     except ImportError as e:
         raise RuntimeError(f"the marshalling module does not load ({e}): build it with `python -m paper_2604_10103_amd.build`") from e
     _marshal.bind({name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _marshal.entry_names()}, HFError,
-                  hf_config, hf_window, hf_ring)
+                  hf_config, hf_window, hf_ring, hf_rope_axes, hf_paged)
     _lib, _native = lib, _marshal
     return lib
 
@@ -405,3 +443,29 @@ def hf_hybrid_attn_bwd_saved(cfg: hf_config, Q, K_win, V_win, block_idx, state, 
     """hf_hybrid_attn_bwd from O_local and lse2 as hf_hybrid_attn_fwd_save wrote them (no recomputed forward)."""
     _call().hybrid_attn_bwd_saved(cfg, Q, K_win, V_win, block_idx, state, dO, O_local, lse2, dQ, dK, dV, workspace, rope_cos_q,
                                   rope_sin_q, Q_hist, dQ_hist, n_kv)
+
+
+def hf_rope_axes_apply(rope: hf_rope_axes, X, positions, Y, inverse: bool = False) -> None:
+    """Y = X with every pair turned by its token's positions; inverse: the other way, the gradient of the forward call.
+    X, Y: [batch, heads, tokens, head_dim] or packed [tokens, heads, head_dim], strided views too (the last dimension contiguous,
+    the other strides multiples of 16 bytes); Y may be X.  positions: int32 [axes, tokens] or [batch, axes, tokens]."""
+    _call().rope_axes_apply(rope, X, positions, Y, inverse)
+
+
+def hf_paged_append(cache: hf_paged, K_new, V_new, cu_new, seq_lens, K_pages, V_pages, page_table, rope=None, positions=None, Q=None,
+                    Q_out=None) -> None:
+    """New keys, rotated (rope None: copied), and values [rows, heads_kv, head_dim] enter the pages of their sequences; Q [rows, heads,
+    head_dim] is rotated into Q_out (may be Q) in the same launch.  positions None: a token's place in its sequence on every axis.
+    cu_new: int32 [n_seqs + 1]; seq_lens: int32 [n_seqs], the new tokens included; page_table: int32 [n_seqs, max_pages]."""
+    _call().paged_append(cache, K_new, V_new, cu_new, seq_lens, K_pages, V_pages, page_table, rope, positions, Q, Q_out)
+
+
+def hf_paged_workspace_bytes(cache: hf_paged, n_q: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().hf_paged_workspace_bytes(ctypes.byref(cache), n_q, ctypes.byref(out)))
+    return out.value
+
+
+def hf_paged_attn_fwd(cache: hf_paged, Q, cu_new, seq_lens, K_pages, V_pages, page_table, O, workspace=None, lse2=None) -> None:
+    """Attention of every sequence's new tokens Q [rows, heads, head_dim] over its pages; lse2: optional fp32 [heads, rows] out."""
+    _call().paged_attn_fwd(cache, Q, cu_new, seq_lens, K_pages, V_pages, page_table, O, workspace, lse2)

@@ -32,6 +32,9 @@ SOURCES = [
     "hf_attn_w64.hip",
     "hf_readout_mfma.hip",
     "hf_rope.hip",
+    "hf_rope_axes.hip",
+    "hf_paged_attn.hip",
+    "hf_api_paged.hip",
     "hf_bwd.hip",
     "hf_bwd_mfma.hip",
     "hf_probe.hip",

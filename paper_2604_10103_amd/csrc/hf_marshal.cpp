@@ -24,7 +24,8 @@ namespace {
   X(hf_block_select_static) X(hf_hybrid_attn_fwd) X(hf_hybrid_attn_fwd_split) X(hf_hybrid_attn_fwd_planes) X(hf_pool_keys)  \
   X(hf_select_attn_fwd) X(hf_step_fwd) X(hf_hybrid_attn_fwd_save) X(hf_rope_window_indices) X(hf_rope_tables)               \
   X(hf_rope_append_keys) X(hf_rope_apply) X(hf_stream_open_chunk) X(hf_stream_step) X(hf_ring_open_chunk) X(hf_ring_step)   \
-  X(hf_ring_last_step) X(hf_hybrid_attn_bwd) X(hf_hybrid_attn_bwd_saved)
+  X(hf_ring_last_step) X(hf_hybrid_attn_bwd) X(hf_hybrid_attn_bwd_saved) X(hf_rope_axes_apply) X(hf_paged_append)           \
+  X(hf_paged_attn_fwd) X(hf_paged_workspace_bytes)
 
 #define HF_POINTER(name) decltype(&::name) name = nullptr;
 struct {
@@ -504,7 +505,134 @@ PyObject* hybrid_attn_bwd_saved(Args a) {
   return none();
 }
 
-// bind(addresses by name, HFError, hf_config, hf_window, hf_ring)
+// ---- rotation by positions and the cache of pages: strided operands, whose device has to be the current one
+struct Strided {
+  void* p = nullptr;
+  int64_t n[3] = {0, 0, 0}, stride[3] = {0, 0, 0};   // the outer dimensions
+  const int64_t* strides() const { return stride; }
+};
+
+void on_current_device(const at::Tensor& t, const char* name) {
+  if (t.get_device() != c10::hip::current_device())
+    raise(PyExc_ValueError, "%s is on device %d, the current one is %d", name, (int)t.get_device(), (int)c10::hip::current_device());
+}
+
+void* here(PyObject* o, const char* name, at::ScalarType type, Shape shape) {   // contiguous
+  void* p = ptr(o, name, type, shape);
+  if (o != Py_None) on_current_device(THPVariable_Unpack(o), name);
+  return p;
+}
+
+Strided strided(PyObject* o, const char* name, at::ScalarType type, int outer) {
+  Strided s;
+  if (o == Py_None) return s;
+  const at::Tensor& t = tensor(o, name);
+  if (!t.is_cuda()) raise(PyExc_TypeError, "%s must be a GPU tensor", name);
+  if (t.scalar_type() != type) raise(PyExc_TypeError, "%s must be %s, got %s", name, dtype_name(type), dtype_name(t.scalar_type()));
+  if (t.dim() != outer + 1) raise(PyExc_ValueError, "%s must have %d dimensions, got %d", name, outer + 1, (int)t.dim());
+  if (t.size(outer) > 1 && t.stride(outer) != 1) raise(PyExc_ValueError, "the last dimension of %s must be contiguous", name);
+  on_current_device(t, name);
+  for (int i = 0; i < outer; ++i) {
+    s.n[i] = t.size(i);
+    s.stride[i] = t.size(i) > 1 ? t.stride(i) : 0;
+  }
+  s.p = t.data_ptr();
+  return s;
+}
+
+void same_shape(PyObject* o, const char* name, Shape shape) {
+  if (o == Py_None) return;
+  const at::IntArrayRef got = THPVariable_Unpack(o).sizes(), want(shape.begin(), shape.size());
+  if (got != want) raise(PyExc_ValueError, "%s must have shape %s, got %s", name, text(want).c_str(), text(got).c_str());
+}
+
+at::ScalarType type_of(int32_t dtype) { return dtype == HF_F32 ? at::kFloat : at::kBFloat16; }   // (the library refuses others)
+
+PyObject* rope_axes_apply(Args a) {   // rope, X, positions, Y, inverse
+  const Struct<hf_rope_axes> rope(a[0], "hf_rope_axes");
+  const at::Tensor& x = tensor(a[1], "X");
+  const at::ScalarType type = x.scalar_type() == at::kFloat ? at::kFloat : at::kBFloat16;
+  const int dims = (int)x.dim();
+  if (dims != 3 && dims != 4) raise(PyExc_ValueError, "X must be [batch, heads, tokens, head_dim] or [tokens, heads, head_dim], got %d dimensions", dims);
+  Strided xs = strided(a[1], "X", type, dims - 1), ys = strided(a[3], "Y", type, dims - 1);
+  const int64_t d = x.size(dims - 1);
+  same_shape(a[3], "Y", dims == 4 ? Shape{xs.n[0], xs.n[1], xs.n[2], d} : Shape{xs.n[0], xs.n[1], d});
+  if (dims == 3)   // packed: one batch, heads before tokens
+    for (Strided* s : {&xs, &ys}) {
+      s->n[2] = s->n[0]; s->stride[2] = s->stride[0];
+      s->n[0] = 1; s->stride[0] = 0;
+    }
+  const int64_t B = xs.n[0], n = xs.n[2], axes = rope->n_axes;
+  const at::Tensor& pos = tensor(a[2], "positions");
+  const bool per_batch = pos.dim() == 3;
+  void* p = per_batch ? here(a[2], "positions", at::kInt, {B, axes, n}) : here(a[2], "positions", at::kInt, {axes, n});
+  const int inverse = PyObject_IsTrue(a[4]);
+  if (inverse < 0) throw Raised();
+  for (int64_t v : {B, xs.n[1], n, d})
+    if (v > INT32_MAX) raise(PyExc_OverflowError, "%lld does not fit in 32 bits", (long long)v);
+  call{lib.hf_rope_axes_apply, rope.get(), type == at::kFloat ? (int)HF_F32 : (int)HF_BF16, (int)d, (int)B, (int)xs.n[1], (int)n, xs.p,
+       xs.strides(), static_cast<const int32_t*>(p), (int)per_batch, ys.p, ys.strides(), inverse, stream()};
+  return none();
+}
+
+struct Paged : Struct<hf_paged> {
+  at::ScalarType type;
+  explicit Paged(PyObject* o) : Struct(o, "hf_paged") {
+    type = type_of(get()->dtype);
+    size_t n = 0;
+    check(lib.hf_paged_workspace_bytes(get(), 0, &n));   // the library's own refusals come first
+  }
+  Strided rows(PyObject* o, const char* name, int64_t n, int64_t heads) const {
+    Strided s = strided(o, name, type, 2);
+    same_shape(o, name, {n, heads, get()->head_dim});
+    return s;
+  }
+  void* pages(PyObject* o, const char* name) const {
+    return here(o, name, type, {get()->n_pages, get()->heads_kv, get()->page_tokens, get()->head_dim});
+  }
+  const int32_t* ints(PyObject* o, const char* name, Shape shape) const { return static_cast<const int32_t*>(here(o, name, at::kInt, shape)); }
+};
+
+int rows_of(PyObject* o, const char* name) {
+  const int64_t n = length(o, name, 0, 3);
+  if (n > INT32_MAX) raise(PyExc_OverflowError, "%lld does not fit in 32 bits", (long long)n);
+  return (int)n;
+}
+
+PyObject* paged_append(Args a) {   // cache, K_new, V_new, cu_new, seq_lens, K_pages, V_pages, page_table, rope, positions, Q, Q_out
+  const Paged c(a[0]);
+  const int n = rows_of(a[1], "K_new");
+  const Strided k = c.rows(a[1], "K_new", n, c->heads_kv), v = c.rows(a[2], "V_new", n, c->heads_kv);
+  const int32_t *cu = c.ints(a[3], "cu_new", {c->n_seqs + 1}), *lens = c.ints(a[4], "seq_lens", {c->n_seqs});
+  void *kp = c.pages(a[5], "K_pages"), *vp = c.pages(a[6], "V_pages");
+  const int32_t* table = c.ints(a[7], "page_table", {c->n_seqs, c->max_pages});
+  hf_rope_axes rope = {};
+  const bool turns = a[8] != Py_None;
+  if (turns) rope = *Struct<hf_rope_axes>(a[8], "hf_rope_axes").get();
+  else if (a[9] != Py_None) raise(PyExc_ValueError, "positions without rope");
+  const int32_t* pos = c.ints(a[9], "positions", {rope.n_axes, n});
+  const Strided q = c.rows(a[10], "Q", n, c->heads), o = c.rows(a[11], "Q_out", n, c->heads);
+  call{lib.hf_paged_append, c.get(), turns ? &rope : nullptr, n, k.p, k.strides(), v.p, v.strides(), q.p, q.strides(), cu, lens, pos,
+       kp, vp, table, o.p, o.strides(), stream()};
+  return none();
+}
+
+PyObject* paged_attn_fwd(Args a) {   // cache, Q, cu_new, seq_lens, K_pages, V_pages, page_table, O, workspace, lse2
+  const Paged c(a[0]);
+  const int n = rows_of(a[1], "Q");
+  const Strided q = c.rows(a[1], "Q", n, c->heads);
+  const int32_t *cu = c.ints(a[2], "cu_new", {c->n_seqs + 1}), *lens = c.ints(a[3], "seq_lens", {c->n_seqs});
+  void *kp = c.pages(a[4], "K_pages"), *vp = c.pages(a[5], "V_pages");
+  const int32_t* table = c.ints(a[6], "page_table", {c->n_seqs, c->max_pages});
+  const Strided o = c.rows(a[7], "O", n, c->heads);
+  void* ws = bytes(a[8], "workspace");
+  if (a[8] != Py_None) on_current_device(THPVariable_Unpack(a[8]), "workspace");
+  float* lse = static_cast<float*>(here(a[9], "lse2", at::kFloat, {c->heads, n}));
+  call{lib.hf_paged_attn_fwd, c.get(), q.p, q.strides(), n, cu, lens, kp, vp, table, o.p, o.strides(), lse, ws, size_of(a[8]), stream()};
+  return none();
+}
+
+// bind(addresses by name, HFError, hf_config, hf_window, hf_ring, hf_rope_axes, hf_paged)
 PyObject* bind(Args a) {
   if (!PyDict_Check(a[0])) raise(PyExc_TypeError, "bind takes a dict of addresses");
   auto address = [&](const char* name) -> void* {
@@ -524,6 +652,8 @@ PyObject* bind(Args a) {
   Class<hf_config>::type = structure(a[2]);
   Class<hf_window>::type = structure(a[3]);
   Class<hf_ring>::type = structure(a[4]);
+  Class<hf_rope_axes>::type = structure(a[5]);
+  Class<hf_paged>::type = structure(a[6]);
   Py_INCREF(a[1]);
   Py_XDECREF(error_class);
   error_class = a[1];
@@ -556,14 +686,15 @@ template <PyObject* (*F)(Args), int N> PyObject* method(PyObject*, PyObject* con
 
 #define HF_METHOD(name, n) {#name, (PyCFunction)(void*)(&method<name, n>), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
-    HF_METHOD(bind, 5), HF_METHOD(entry_names, 0), HF_METHOD(state_init, 2), HF_METHOD(state_fold_linear, 4),
+    HF_METHOD(bind, 7), HF_METHOD(entry_names, 0), HF_METHOD(state_init, 2), HF_METHOD(state_fold_linear, 4),
     HF_METHOD(state_planes, 3), HF_METHOD(absorb_evicted, 7), HF_METHOD(absorb_evicted_planes, 8), HF_METHOD(window_evict, 10),
     HF_METHOD(block_select, 8), HF_METHOD(block_select_static, 6), HF_METHOD(hybrid_attn_fwd, 12),
     HF_METHOD(hybrid_attn_fwd_planes, 12), HF_METHOD(hybrid_attn_fwd_save, 14), HF_METHOD(pool_keys, 5),
     HF_METHOD(select_attn_fwd, 14), HF_METHOD(step_fwd, 20), HF_METHOD(rope_window_indices, 3), HF_METHOD(rope_tables, 8),
     HF_METHOD(rope_append_keys, 8), HF_METHOD(rope_apply, 5), HF_METHOD(stream_open_chunk, 9), HF_METHOD(stream_step, 13),
     HF_METHOD(ring_open_chunk, 8), HF_METHOD(ring_step, 13), HF_METHOD(ring_last_step, 17), HF_METHOD(hybrid_attn_bwd, 16),
-    HF_METHOD(hybrid_attn_bwd_saved, 18), {nullptr, nullptr, 0, nullptr}};
+    HF_METHOD(hybrid_attn_bwd_saved, 18), HF_METHOD(rope_axes_apply, 5), HF_METHOD(paged_append, 12), HF_METHOD(paged_attn_fwd, 10),
+    {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "argument marshalling of the hf library", -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,339 @@
+"""The cache of pages: new tokens enter it, and attention reads it; against the 64-bit oracle, element by element (bounds: tests/paged.py)."""
+import numpy as np
+import pytest
+import torch
+
+import oracle.paged as orc
+import paper_2604_10103_amd as hf
+from paged import DEV, TYPES, Batch, f64
+
+pytestmark = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------------------------------------------- append
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("page", [1, 7, 16, 40])
+@pytest.mark.parametrize("form", ["plain", "place", "adjacent", "halves", "odd"])
+def test_appended_tokens_lie_in_their_pages(dtype, d, page, form):
+    new, lens = [1, 0, 5, 33, 1, 3], [1, 9, 5, 70, 17, 2]     # the last one's first token lies before the sequence
+    b = Batch(new, lens, 6, 2, d, dtype, page, rows_behind=4, seed=page + d)
+    b.table[2, 0] = b.n_pages + 3                              # no page: dropped
+    b.to_gpu()
+    pairs = {"plain": None, "place": [d // 2], "adjacent": [d // 2 - 2 * (d // 6), d // 6, d // 6], "halves": [d // 4, d // 8, d // 8],
+             "odd": [5, 4]}[form]
+    rope = pos = None
+    if pairs:
+        rope = hf.make_rope_axes(pairs, layout=hf.HF_ROPE_ADJACENT if form == "adjacent" else hf.HF_ROPE_HALVES)
+        if form != "place":
+            pos = torch.randint(0, 900, (len(pairs), b.n), generator=torch.Generator().manual_seed(1), dtype=torch.int32).to(DEV)
+    places = np.concatenate([np.arange(n - m, n) for m, n in zip(new, lens)] + [np.zeros(4, dtype=int)])
+    turned = {}
+    for name, x in (("K", b.K), ("Q", b.Q)):
+        if pairs:   # what hf_rope_axes_apply writes, to the bit
+            y = torch.empty((b.n, x.shape[1], d), dtype=b.t, device=DEV)
+            p = pos if pos is not None else torch.tensor(places, dtype=torch.int32, device=DEV)[None]
+            hf.hf_rope_axes_apply(rope, x, p, y)
+            turned[name] = y
+        else:
+            turned[name] = x.clone()
+    want_K, want_V = orc.append(f64(b.K_pages), f64(b.V_pages), f64(turned["K"]), f64(b.V), b.cu, b.lens, b.table)
+    keep_K, keep_V = b.K_pages.clone(), b.V_pages.clone()
+    Q_out = torch.full((b.n, 6, d), 7.0, dtype=b.t, device=DEV)
+    hf.hf_paged_append(b.cache, b.K, b.V, b.cu_d, b.lens_d, b.K_pages, b.V_pages, b.table_d, rope=rope, positions=pos, Q=b.Q, Q_out=Q_out)
+    assert np.array_equal(f64(b.K_pages), want_K) and np.array_equal(f64(b.V_pages), want_V)
+    assert torch.equal(Q_out[:-4], turned["Q"][:-4]) and (Q_out[-4:] == 7.0).all()
+    # without queries, and with queries turned where they lie
+    b.K_pages.copy_(keep_K)
+    b.V_pages.copy_(keep_V)
+    hf.hf_paged_append(b.cache, b.K, b.V, b.cu_d, b.lens_d, b.K_pages, b.V_pages, b.table_d, rope=rope, positions=pos)
+    assert np.array_equal(f64(b.K_pages), want_K) and np.array_equal(f64(b.V_pages), want_V)
+    K, V = b.K.clone(), b.V.clone()
+    hf.hf_paged_append(b.cache, b.K, b.V, b.cu_d, b.lens_d, b.K_pages, b.V_pages, b.table_d, rope=rope, positions=pos, Q=b.Q, Q_out=b.Q)
+    assert torch.equal(b.Q[:-4], turned["Q"][:-4]) and torch.equal(b.K, K) and torch.equal(b.V, V)
+
+
+def test_many_sequences_find_their_rows():
+    rng = np.random.default_rng(0)
+    new = rng.choice([0, 1, 1, 2, 5], size=700)
+    lens = new + rng.integers(0, 20, size=700)
+    b = Batch(new, lens, 2, 1, 64, "bf16", 16, seed=3)
+    want_K, want_V = orc.append(f64(b.K_pages), f64(b.V_pages), f64(b.K), f64(b.V), b.cu, b.lens, b.table)
+    hf.hf_paged_append(b.cache, b.K, b.V, b.cu_d, b.lens_d, b.K_pages, b.V_pages, b.table_d)
+    assert np.array_equal(f64(b.K_pages), want_K) and np.array_equal(f64(b.V_pages), want_V)
+
+
+def test_values_that_are_copied_keep_every_bit():
+    b = Batch([3], [3], 1, 1, 64, "bf16", 4)
+    bits = torch.randint(-32768, 32767, (3, 1, 64), generator=torch.Generator().manual_seed(2), dtype=torch.int32).to(torch.int16).to(DEV)
+    V = bits.view(torch.bfloat16)                              # NaNs of every kind among them
+    hf.hf_paged_append(b.cache, b.K, V, b.cu_d, b.lens_d, b.K_pages, b.V_pages, b.table_d, rope=hf.make_rope_axes([32]))
+    assert torch.equal(b.V_pages[int(b.table[0, 0])].transpose(0, 1)[:3].view(torch.int16), bits)
+
+
+# ---------------------------------------------------------------------------------------------------- attention
+MASKS = [dict(), dict(causal=False), dict(window=9), dict(window=30, n_sink=3), dict(causal=False, window=50, n_sink=17),
+         dict(window=1), dict(causal=False, window=5)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("mask", MASKS)
+def test_single_tokens(dtype, d, mask):
+    lens = [1, 2, 31, 32, 33, 0, 64, 65, 200, 517, 1000]
+    b = Batch([1] * len(lens), lens, 8, 2, d, dtype, 16, seed=d, **mask)
+    b.check(*b.attend())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("mask", MASKS)
+def test_chunks_and_single_tokens_in_one_batch(dtype, d, mask):
+    new, lens = [40, 1, 0, 17, 130, 3], [40, 77, 12, 300, 131, 3]
+    b = Batch(new, lens, 6, 2, d, dtype, 40, rows_behind=5, seed=d + 1, **mask)
+    b.check(*b.attend())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("page", [1, 2, 3, 8, 15, 16, 24, 31, 32, 33, 100, 128, 1560])
+def test_pages_of_any_size(dtype, page):
+    b = Batch([1, 45, 2], [97, 150, 1], 4, 2, 128, dtype, page, seed=page)
+    b.check(*b.attend())
+    b = Batch([5, 1], [150, 33], 4, 2, 64, dtype, page, causal=False, window=70, n_sink=5, seed=page)
+    b.check(*b.attend())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,heads_kv", [(1, 1), (3, 3), (5, 1), (16, 1), (33, 1), (70, 2), (40, 8), (12, 12)])
+def test_groups_of_heads(dtype, heads, heads_kv):
+    b = Batch([1, 2, 9], [40, 100, 9], heads, heads_kv, 64, dtype, 16, seed=heads)
+    b.check(*b.attend())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_long_contexts_are_shared_out(dtype, d):
+    """Enough keys that several workgroups share a row's."""
+    b = Batch([1, 2, 1], [20000, 9001, 5], 4, 2, d, dtype, 64, seed=7)
+    b.check(*b.attend())
+    b = Batch([150], [6000], 2, 1, d, dtype, 64, seed=8)
+    b.check(*b.attend())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("gain", [30.0])
+def test_sharp_softmax_rescales(dtype, gain):
+    b = Batch([1, 60, 1], [700, 333, 3000], 4, 2, 128, dtype, 32, gain=gain, seed=9)
+    b.check(*b.attend())
+
+
+@pytest.mark.parametrize("scale", [0.25, 1e-3])
+def test_softmax_scale(scale):
+    b = Batch([1, 20], [90, 50], 4, 4, 64, "bf16", 16, scale=scale, seed=10)
+    b.check(*b.attend())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_without_a_key(dtype):
+    """New tokens before the sequence (more of them than its length), empty sequences, pages that are none."""
+    b = Batch([6, 1, 2, 40], [3, 0, 40, 40], 4, 2, 64, dtype, 8, rows_behind=3, seed=11, extra_entries=1)
+    b.table[2, :] = -1
+    b.table[3, 1] = b.n_pages
+    b.table[3, 3] = -(2 ** 31)
+    b.to_gpu()
+    b.check(*b.attend())
+    b.cache.causal = 0
+    b.mask["causal"] = False
+    b.check(*b.attend())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("mask", [dict(), dict(window=20, n_sink=4), dict(causal=False)])
+@pytest.mark.parametrize("new,n", [(70, 70), (150, 200), (3, 90), (1, 64)])
+def test_what_is_not_seen_does_not_count(dtype, d, bad, mask, new, n):
+    """Keys and values that are not finite reach the rows that see them and no others, beyond the length included."""
+    b = Batch([new, 1], [n, 50], 4, 2, d, dtype, 24, seed=12, **mask)
+    b.check(*b.attend())
+    ref = b.oracle()
+    clean, clean_lse = b.attend()
+    where = [j for j in {n - 1, n - new + new // 2, n - new // 3, max(0, n - 40)} if 0 <= j < n]
+    for pages in (b.K_pages, b.V_pages):
+        for j in where:
+            pages[int(b.table[0, j // 24]), :, j % 24, :5] = bad
+        for s, length in ((0, n), (1, 50)):                    # what lies behind the length in its last page
+            if length % 24:
+                pages[int(b.table[s, length // 24]), :, length % 24:] = bad
+        for spare in set(range(b.n_pages)) - set(b.table.flatten().tolist()):
+            pages[spare] = bad
+    O, lse = b.attend()
+    hit = np.zeros(b.n, dtype=bool)
+    for i in range(new):
+        seen = orc.sees(n - new + i, n, **b.mask)
+        hit[i] = any(seen[j] for j in where)
+    untouched = torch.tensor(~hit, device=DEV)
+    assert torch.equal(O[untouched], clean[untouched]) and torch.equal(lse[:, untouched], clean_lse[:, untouched])
+    if hit.any():
+        # a key that is not finite gives NaN, +inf or -inf as a score: in the rows that see it nothing can be asserted but that a NaN
+        # key makes the whole row NaN
+        rows = torch.tensor(hit, device=DEV)
+        if bad != bad:
+            assert torch.isnan(O[rows]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_values_that_are_not_finite_reach_their_features(dtype, d, bad):
+    """Values alone: a visible one makes its own feature NaN or that infinity, the others stay within their bounds."""
+    new, n = 100, 140
+    b = Batch([new], [n], 4, 2, d, dtype, 24, window=50, n_sink=2, seed=13)
+    ref = b.oracle()
+    where = {90: 3, 120: d - 1, 139: 17, 45: 40}
+    for j, f in where.items():
+        b.V_pages[int(b.table[0, j // 24]), :, j % 24, f] = bad
+    O, lse = b.attend()
+    got, fine = f64(O), np.ones((new, d), dtype=bool)
+    for i in range(new):
+        seen = orc.sees(n - new + i, n, **b.mask)
+        for j, f in where.items():
+            if seen[j]:
+                fine[i, f] = False
+                assert all(np.isnan(x) if bad != bad else (x == bad or np.isnan(x)) for x in got[i, :, f])
+    for h in range(4):
+        o, r = got[:, h][fine], ref[0][:, h][fine]
+        assert np.isfinite(o).all() and np.abs(o - r).max() <= (2e-2 if dtype == "bf16" else 1e-5) * np.abs(ref[2]).max()
+    b.check(torch.tensor(np.where(fine[:, None], got, ref[0]), device=DEV), lse, ref)
+
+
+def test_the_same_bits_every_time_and_in_any_workspace():
+    b = Batch([1] * 30 + [70], list(range(1, 6000, 200)) + [900], 8, 2, 128, "bf16", 16, seed=14)
+    O, lse = b.attend()
+    n = max(1, hf.hf_paged_workspace_bytes(b.cache, b.n))
+    for fill in (0, 255, 1):
+        O2, lse2 = b.attend(workspace=torch.full((n,), fill, dtype=torch.uint8, device=DEV))
+        assert torch.equal(O, O2) and torch.equal(lse, lse2)
+    ws = torch.zeros(n, dtype=torch.uint8, device=DEV)
+    for _ in range(5):   # the same workspace again and again
+        O2, lse2 = b.attend(workspace=ws)
+        assert torch.equal(O, O2) and torch.equal(lse, lse2)
+
+
+def test_sequences_share_pages_and_come_in_any_order():
+    b = Batch([4, 4, 4], [100, 100, 100], 4, 2, 64, "bf16", 16, seed=15)
+    b.table[1, :6] = b.table[0, :6]                            # a common beginning of 96 tokens
+    b.table[2] = b.table[0]
+    b.to_gpu()
+    b.check(*b.attend())
+
+
+def test_strided_operands():
+    b = Batch([3, 40, 1], [30, 60, 200], 6, 3, 128, "bf16", 16, seed=16)
+    want, _ = b.attend()
+    wide = torch.full((6, b.n, 136), 7.0, dtype=torch.bfloat16, device=DEV)
+    O, _ = b.attend(O=wide[:, :, :128].transpose(0, 1))
+    assert torch.equal(O, want) and (wide[:, :, 128:] == 7.0).all()
+    b.Q = b.Q.transpose(0, 1).contiguous().transpose(0, 1)
+    O, _ = b.attend()
+    assert torch.equal(O, want)
+
+
+def test_another_stream():
+    b = Batch([1, 50], [3000, 400], 8, 2, 128, "bf16", 16, seed=17)
+    want, lse = b.attend()
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        O, lse2 = b.attend()
+    s.synchronize()
+    assert torch.equal(O, want) and torch.equal(lse, lse2)
+
+
+def test_no_rows():
+    b = Batch([0, 0], [5, 9], 4, 2, 64, "bf16", 16)
+    O, lse = b.attend()
+    hf.hf_paged_append(b.cache, b.K, b.V, b.cu_d, b.lens_d, b.K_pages, b.V_pages, b.table_d)
+
+
+# ---------------------------------------------------------------------------------------------------- together
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("causal,window,sink,page,pairs,halves", [(True, 0, 0, 16, [64], True), (False, 90, 30, 30, [22, 21, 21], False)])
+def test_sequences_grow_step_by_step(dtype, causal, window, sink, page, pairs, halves):
+    """Prompts (or chunks of frames), then single tokens, in one captured step for all of them: every step against attention over the
+    whole history, rotated by the oracle."""
+    S, H, Hk, d, steps = 3, 4, 2, 128, 5
+    first = [37, 1, 64]
+    b = Batch(first, first, H, Hk, d, dtype, page, causal=causal, window=window, n_sink=sink, seed=18)
+    width = -(-(max(first) + steps) // page)
+    b.n_pages = S * width
+    b.table = np.random.default_rng(1).permutation(b.n_pages).reshape(S, width).astype(np.int32)
+    b.K_pages = torch.full((b.n_pages, Hk, page, d), float("nan"), dtype=b.t, device=DEV)
+    b.V_pages = b.K_pages.clone()
+    cache = hf.make_paged(H, Hk, d, dtype, page, b.n_pages, S, width, causal=causal, window=window, n_sink=sink)
+    rope = hf.make_rope_axes(pairs, layout=hf.HF_ROPE_HALVES if halves else hf.HF_ROPE_ADJACENT)
+    lens = torch.tensor(first, dtype=torch.int32, device=DEV)
+    table = torch.tensor(b.table, device=DEV)
+    history = [[] for _ in range(S)]
+
+    def place(lens_now, counts):
+        at = np.concatenate([np.arange(n - m, n) for n, m in zip(lens_now, counts)])
+        return np.stack([at // (1 + 3 * a) for a in range(len(pairs))])
+
+    def check(rows, O, cu, lens_now, pos):
+        q = orc.rotate_axes(f64(rows[:, :H]).transpose(1, 0, 2), pos, pairs, halves=halves).transpose(1, 0, 2)
+        k = orc.rotate_axes(f64(rows[:, H:H + Hk]).transpose(1, 0, 2), pos, pairs, halves=halves).transpose(1, 0, 2)
+        v = f64(rows[:, H + Hk:])
+        for s in range(S):
+            for i in range(cu[s], cu[s + 1]):
+                history[s].append((k[i], v[i]))
+        for s in range(S):
+            K, V = np.stack([x[0] for x in history[s]]), np.stack([x[1] for x in history[s]])
+            for i in range(cu[s], cu[s + 1]):
+                ok = orc.sees(lens_now[s] - cu[s + 1] + i, lens_now[s], causal, window, sink)
+                for h in range(H):
+                    logit = K[ok, h // 2] @ q[i, h] / np.sqrt(d)
+                    w = np.exp(logit - logit.max())
+                    ref = w @ V[ok, h // 2] / w.sum()
+                    # rounding of rotated q and k moves a logit by 2 half steps of |q| |k| sizes; then as a bound of tests/paged.py
+                    size = (np.abs(K[ok, h // 2]) @ np.abs(q[i, h])).max() / np.sqrt(d)
+                    half = 2.0 ** -8 if dtype == "bf16" else 6 * 2.0 ** -24
+                    spread = w @ np.abs(V[ok, h // 2]) / w.sum()
+                    assert (np.abs(f64(O[i, h]) - ref) <= half * np.abs(ref) + spread * (half + 4 * half * size + 1e-5)).all()
+
+    ws = torch.empty(max(1, hf.hf_paged_workspace_bytes(cache, b.n)), dtype=torch.uint8, device=DEV)
+    O = torch.empty((b.n, H, d), dtype=b.t, device=DEV)
+    Q = torch.empty_like(O)
+    pos = place(first, first)
+    hf.hf_paged_append(cache, b.K, b.V, b.cu_d, lens, b.K_pages, b.V_pages, table, rope=rope,
+                       positions=torch.tensor(pos, dtype=torch.int32, device=DEV), Q=b.Q, Q_out=Q)
+    hf.hf_paged_attn_fwd(cache, Q, b.cu_d, lens, b.K_pages, b.V_pages, table, O, ws)
+    check(b.rows, O, b.cu, first, pos)
+    # one token each, captured: lengths, positions and tokens are what changes
+    rows = torch.empty((S, H + 2 * Hk, d), dtype=b.t, device=DEV)
+    pos_d, cu = torch.zeros((len(pairs), S), dtype=torch.int32, device=DEV), torch.arange(S + 1, dtype=torch.int32, device=DEV)
+    q1, O1 = torch.empty((S, H, d), dtype=b.t, device=DEV), torch.empty((S, H, d), dtype=b.t, device=DEV)
+    ws1 = torch.empty(max(1, hf.hf_paged_workspace_bytes(cache, S)), dtype=torch.uint8, device=DEV)
+
+    def step():
+        hf.hf_paged_append(cache, rows[:, H:H + Hk], rows[:, H + Hk:], cu, lens, b.K_pages, b.V_pages, table, rope=rope, positions=pos_d,
+                           Q=rows[:, :H], Q_out=q1)
+        hf.hf_paged_attn_fwd(cache, q1, cu, lens, b.K_pages, b.V_pages, table, O1, ws1)
+
+    g, now = None, list(first)
+    for k in range(steps):
+        rows.copy_(torch.randn(rows.shape, generator=torch.Generator().manual_seed(100 + k)).to(b.t))
+        now = [n + 1 for n in now]
+        lens.copy_(torch.tensor(now, dtype=torch.int32))
+        pos = place(now, [1] * S)
+        pos_d.copy_(torch.tensor(pos, dtype=torch.int32))
+        if k == 0:
+            step()
+            torch.cuda.synchronize()
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g):
+                step()
+        else:
+            g.replay()
+        torch.cuda.synchronize()
+        check(rows, O1, list(range(S + 1)), now, pos)
