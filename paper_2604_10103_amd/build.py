@@ -34,6 +34,7 @@ SOURCES = [
     "hf_rope.hip",
     "hf_rope_axes.hip",
     "hf_paged_attn.hip",
+    "hf_paged_attn_f32.hip",
     "hf_api_paged.hip",
     "hf_bwd.hip",
     "hf_bwd_mfma.hip",

@@ -62,6 +62,12 @@ int check_cache(const hf_paged* c) {
   return HF_OK;
 }
 
+int check_attn_rows(const hf_paged* c, int32_t n_q) {
+  HF_TRY(check_rows(n_q, "n_q"));
+  if ((int64_t)n_q * c->heads > (1ll << 30)) { set_error("n_q * heads must be <= 2^30"); return HF_ERR_SHAPE; }
+  return HF_OK;
+}
+
 // A strided operand of up to three outer dimensions (outermost first) and rows of `row` elements
 struct View {
   const char* p;
@@ -219,7 +225,7 @@ int hf_paged_append(const hf_paged* cache, const hf_rope_axes* rope_or_null, int
 int hf_paged_workspace_bytes(const hf_paged* cache, int32_t n_q, size_t* bytes_out) {
   HF_TRY(check_cache(cache));
   if (!bytes_out) { set_error("bytes_out is NULL"); return HF_ERR_NULL; }
-  HF_TRY(check_rows(n_q, "n_q"));
+  HF_TRY(check_attn_rows(cache, n_q));
   *bytes_out = paged_workspace_bytes(*cache, n_q);
   return HF_OK;
 }
@@ -228,9 +234,8 @@ int hf_paged_attn_fwd(const hf_paged* cache, const void* Q, const int64_t* q_str
                       const int32_t* seq_lens, const void* K_pages, const void* V_pages, const int32_t* page_table, void* O,
                       const int64_t* o_strides, float* lse2_or_null, void* workspace, size_t workspace_bytes, void* stream) {
   HF_TRY(check_cache(cache));
-  HF_TRY(check_rows(n_q, "n_q"));
+  HF_TRY(check_attn_rows(cache, n_q));
   if (n_q == 0) return HF_OK;
-  if ((int64_t)n_q * cache->heads > (1ll << 31)) { set_error("n_q * heads must be <= 2^31"); return HF_ERR_SHAPE; }
   View q = packed(*cache, n_q, cache->heads), o = q;
   HF_TRY(check_packed(q, Q, "Q", q_strides, false));
   HF_TRY(check_pool(cache, K_pages, V_pages, page_table, cu_new, seq_lens));

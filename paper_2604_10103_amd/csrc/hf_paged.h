@@ -19,8 +19,12 @@ struct PagedAttnArgs {
   long long qt, qh, ot, oh;   // strides in elements
   int n_q, heads, heads_kv, page, n_pages, n_seqs, max_pages, causal, window, n_sink;
   float c_scale;              // softmax_scale * log2(e)
+  uint32_t page_magic;        // key / page = key * page_magic >> page_shift for key < 2^31
+  int page_shift;
 };
 size_t paged_workspace_bytes(const hf_paged& c, int n_q);
-int launch_paged_attn(const hf_paged& c, const PagedAttnArgs& a, void* workspace, hipStream_t s);
+int launch_paged_attn(const hf_paged& c, PagedAttnArgs a, void* workspace, hipStream_t s);
+struct PagedSchedule;
+int launch_paged_attn_f32(const hf_paged& c, const PagedAttnArgs& a, const PagedSchedule& sc, int rows, int items, hipStream_t s);
 
 }  // namespace hf

@@ -1,0 +1,226 @@
+// Attention over a cache of pages in fp32 (hf_paged_attn_fwd, fp32 storage): both products on v_mfma_f32_32x32x2_f32.
+//
+// Rows, items and statistics as in hf_paged_attn.hip (the instruction's result has the same layout).  Nothing passes through LDS before
+// the end: a lane reads its key's row in 16-byte pieces (product over features), and of every value row the 16 or 8 bytes whose features
+// are its operands (product over keys), each row by an address of its own, so that pages may end anywhere; a key that is none reads a
+// row of zeros.  The four k indices of a piece feed four instructions; accumulator e holds the features E * (row of the result) + e.
+#include "hf_paged_attn.h"
+
+namespace hf {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+namespace {
+
+__device__ float zero_row_f32[128];
+
+__device__ __forceinline__ bool not_finite(float v) { return (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u; }
+
+template <int D, int NW, int KS>
+__global__ __launch_bounds__(64 * NW * KS, 1) void paged_attn_f32_kernel(const PagedAttnArgs a, const PagedSchedule sc) {
+  constexpr int BM = 32 * NW, NT = 64 * NW * KS, NC = D / 8, E = D / 32;   // 16-byte pieces of a key; features of a lane's piece of a value
+  constexpr int SPAN = BM * (D + 4) + BM * 2;                              // a group's sums and statistics, in floats
+  extern __shared__ __attribute__((aligned(16))) float sums[];
+  typedef float piece __attribute__((ext_vector_type(E)));
+
+  PagedItem it;
+  if (!find_item<BM>(a, sc, blockIdx.x, it)) return;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave_in_wg = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave = wave_in_wg % NW, grp = wave_in_wg / NW;
+  const int l32 = lane & 31, h = lane >> 5, group = a.heads / a.heads_kv;
+
+  const int x_last = it.first + it.rows - 1, x = min(it.first + 32 * wave + l32, x_last), token = x / group;
+  const RowView view = row_view(a, it, token);
+  const bool active = 32 * wave < it.rows;
+  const RowView view_lo = row_view(a, it, min(it.first + 32 * wave, x_last) / group);
+  const RowView view_hi = row_view(a, it, min(it.first + 32 * wave + 31, x_last) / group);
+  f32x4 qf[NC];
+  {
+    const float* q = static_cast<const float*>(a.Q) + (long long)(it.begin + token) * a.qt +
+                     (long long)(it.head_kv * group + (x - token * group)) * a.qh + 4 * h;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) qf[c] = *reinterpret_cast<const f32x4*>(q + 8 * c);
+  }
+  f32x16 o[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[e][r] = 0.0f;
+  float m_ref = -INFINITY, l_run = 0.0f;
+  uint32_t seen = 0;
+
+  const bool bad_pages = any_bad_page(a, it);
+  const int count = active ? max(0, (it.t1 - it.t0 - grp + KS - 1) / KS) : 0;
+  auto start_of = [&](int i) { return it.keys.start(it.t0 + grp + KS * i); };
+  auto some_of = [&](int start) { return start < view_hi.hi && (start + kKeyTile > view_lo.lo || start < view.sink); };
+  auto all_of = [&](int start) {
+    return start + kKeyTile <= view_lo.hi && (start >= view_hi.lo || start + kKeyTile <= view.sink) && !bad_pages;
+  };
+  // the lane's key of a tile: its page (-1: none, or past the cache)
+  const int32_t* const table = a.table + (long long)it.seq * a.max_pages;
+  auto page_of = [&](int i) {
+    const int key = i < count ? start_of(i) + l32 : it.held;
+    const int id = table[div_page(a, min(key, max(it.held - 1, 0)))];
+    return key < it.held && is_page(a, id) ? id : -1;
+  };
+  const long long page_rows = (long long)a.heads_kv * a.page, head_row = (long long)it.head_kv * a.page;
+  auto offset_of = [&](int i, int id) {   // element offset in the pool
+    const int key = start_of(i) + l32;
+    return (id * page_rows + head_row + (key - div_page(a, key) * a.page)) * D;
+  };
+  auto load_keys = [&](f32x4 (&k)[NC], int i, int id) {
+    const float* p = (id >= 0 ? static_cast<const float*>(a.K_pages) + offset_of(i, id) : zero_row_f32) + 4 * h;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) k[c] = *reinterpret_cast<const f32x4*>(p + 8 * c);
+  };
+  int id = -1, id_next = -1;
+  f32x4 kf[NC];
+  if (count > 0) {
+    id = page_of(0);
+    id_next = page_of(1);
+    load_keys(kf, 0, id);
+  }
+  bool odd = false;   // values that are not finite lie next to rows that do not see them: they were left out (uniform)
+
+  for (int i = 0; i < count; ++i) {
+    const int start = start_of(i);
+    const uint32_t exists = (uint32_t)__ballot(id >= 0);
+    const float* const v_row = id >= 0 ? static_cast<const float*>(a.V_pages) + offset_of(i, id) : zero_row_f32;
+    auto row_of = [&](int key) {   // of the tile
+      return reinterpret_cast<const float*>(__shfl((unsigned long long)reinterpret_cast<uintptr_t>(v_row), key, kWave));
+    };
+    const int id_after = page_of(i + 2);
+    if (some_of(start)) {
+      piece vf[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) vf[r] = *reinterpret_cast<const piece*>(row_of(8 * (r >> 2) + 4 * h + (r & 3)) + E * l32);
+      f32x16 sacc;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sacc[r] = 0.0f;
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sacc = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[c][e], qf[c][e], sacc, 0, 0, 0);
+      if (i + 1 < count) load_keys(kf, i + 1, id_next);
+      if (!all_of(start)) {
+        const uint32_t sees = view.sees_tile(start) & exists, mine = sees >> (4 * h);
+        seen |= sees;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sacc[r] = masked_score(sacc[r], mine, 8 * (r >> 2) + (r & 3));
+        uint32_t cut = 0;   // a probability of zero does not make a NaN or an infinity vanish: such values become zero here
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            const uint32_t w = __float_as_uint(vf[r][e]), left = 0x7f800000u - (w & 0x7f800000u);
+            const uint32_t keep = 0u - min(left, 1u);   // all ones where finite
+            cut |= ~keep;
+            vf[r][e] = __uint_as_float(w & keep);
+          }
+        odd = odd || __any(cut != 0);
+      } else {
+        seen = 1;
+      }
+      float mx = sacc[0];
+#pragma unroll
+      for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sacc[r]);
+      mx = fmaxf(mx, __shfl_xor(mx, 32, kWave)) * a.c_scale;
+      const bool grows = mx > m_ref;
+      if (__any(grows)) {
+        const float m_new = grows ? mx : m_ref;
+        const float alpha = grows ? __builtin_amdgcn_exp2f(m_ref - m_new) : 1.0f;
+        m_ref = m_new;
+        l_run *= alpha;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[e][r] *= alpha;
+      }
+      const float m_use = m_ref == -INFINITY ? 0.0f : m_ref;
+      float psum = 0.0f;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        sacc[r] = __builtin_amdgcn_exp2f(fmaf(sacc[r], a.c_scale, -m_use));
+        psum += sacc[r];
+      }
+      l_run += psum;
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[r][e], sacc[r], o[e], 0, 0, 0);
+    } else if (i + 1 < count) {
+      load_keys(kf, i + 1, id_next);
+    }
+    id = id_next;
+    id_next = id_after;
+  }
+
+  // ---- the values that were left out, in the rows that see them: infinite, or NaN next to a probability of zero
+  if (odd) {
+    const float m_use = m_ref == -INFINITY ? 0.0f : m_ref;
+#pragma unroll 1
+    for (int i = 0; i < count; ++i) {
+      const int start = start_of(i);
+      if (!some_of(start) || all_of(start)) continue;
+#pragma unroll 1
+      for (int k = 0; k < kKeyTile; ++k) {
+        const int key = start + k;
+        if (key >= it.held) break;
+        const int entry = div_page(a, key), id = table[entry];
+        if (!is_page(a, id)) continue;
+        const long long at = (id * page_rows + head_row + (key - entry * a.page)) * D;
+        const float *kr = static_cast<const float*>(a.K_pages) + at, *vr = static_cast<const float*>(a.V_pages) + at;
+        float s = 0.0f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const f32x4 w = *reinterpret_cast<const f32x4*>(kr + 8 * c + 4 * h);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s = fmaf(w[e], qf[c][e], s);
+        }
+        s += __shfl_xor(s, 32, kWave);
+        const bool sees = view.sees(key), positive = __builtin_amdgcn_exp2f(fmaf(s, a.c_scale, -m_use)) > 0.0f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const piece w = *reinterpret_cast<const piece*>(vr + E * (8 * (r >> 2) + 4 * h + (r & 3)));
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            if (sees && not_finite(w[e])) o[e][r] += positive ? w[e] : __builtin_nanf("");
+        }
+      }
+    }
+  }
+
+  l_run += __shfl_xor(l_run, 32, kWave);
+  if (seen != 0 && m_ref == -INFINITY && l_run == 0.0f) l_run = kOnlyInfinite;
+  float* const row = sums + grp * SPAN + (32 * wave + l32) * (D + 4);
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    piece y;
+#pragma unroll
+    for (int e = 0; e < E; ++e) y[e] = o[e][r];
+    *reinterpret_cast<piece*>(row + E * (8 * (r >> 2) + 4 * h + (r & 3))) = y;
+  }
+  if (h == 0) *reinterpret_cast<float2*>(sums + grp * SPAN + BM * (D + 4) + 2 * (32 * wave + l32)) = make_float2(m_ref, l_run);
+  finish_item<float, D, BM, KS, NT>(a, sc, it, [&](int u) { return sums + u * SPAN; }, [&](int u) { return sums + u * SPAN + BM * (D + 4); },
+                                    reinterpret_cast<int*>(sums + KS * SPAN));
+}
+
+template <int D, int NW, int KS> int launch(const PagedAttnArgs& a, const PagedSchedule& sc, int items, hipStream_t s) {
+  constexpr int kLds = KS * (32 * NW * (D + 4) + 64 * NW) * 4 + 16;
+  static LdsGrant grant;
+  const int rc = grant_lds(grant, reinterpret_cast<const void*>(&paged_attn_f32_kernel<D, NW, KS>), kLds, "hf_paged_attn_fwd");
+  if (rc != HF_OK) return rc;
+  hipLaunchKernelGGL((paged_attn_f32_kernel<D, NW, KS>), dim3(items), dim3(64 * NW * KS), kLds, s, a, sc);
+  return check_launch("hf_paged_attn_fwd");
+}
+
+}  // namespace
+
+int launch_paged_attn_f32(const hf_paged& c, const PagedAttnArgs& a, const PagedSchedule& sc, int rows, int items, hipStream_t s) {
+  if (c.head_dim == 128) return rows == 128 ? launch<128, 4, 1>(a, sc, items, s) : launch<128, 1, 4>(a, sc, items, s);
+  return rows == 128 ? launch<64, 4, 1>(a, sc, items, s) : launch<64, 1, 4>(a, sc, items, s);
+}
+
+}  // namespace hf
