@@ -619,7 +619,7 @@ typedef struct hf_paged {
   int32_t head_dim;       /* 64 or 128 */
   int32_t dtype;          /* HF_BF16 | HF_F32 */
   int32_t page_tokens;    /* 1 .. 65536 */
-  int32_t n_pages;        /* pages of the pool, >= 1 */
+  int32_t n_pages;        /* pages of the pool, >= 1; n_pages * heads_kv * page_tokens < 2^32 */
   int32_t n_seqs;         /* 1 .. 65535 */
   int32_t max_pages;      /* entries of a table row, >= 1; max_pages * page_tokens <= 2^30 */
   int32_t causal;         /* 0: a token sees every token of its sequence (a chunk of frames); else those up to its own place */

@@ -131,9 +131,9 @@ int check_pool(const hf_paged* c, const void* K_pages, const void* V_pages, cons
   HF_TRY(check_ptr(K_pages, "K_pages"));
   HF_TRY(check_ptr(V_pages, "V_pages"));
   HF_TRY(check_ptr(page_table, "page_table", 4));
-  // (a page holds at most 2^16 tokens of 2^16 heads: 2^41 bytes; the pool's own size is the caller's)
-  if ((__int128)c->n_pages * c->heads_kv * c->page_tokens * c->head_dim * 4 > ((__int128)1 << 62)) {
-    set_error("the pool of pages is too large");
+  // (rows of the pool count in 32 bits: 512 GB at least)
+  if ((unsigned __int128)c->n_pages * c->heads_kv * c->page_tokens >= ((unsigned __int128)1 << 32)) {
+    set_error("n_pages * heads_kv * page_tokens must be < 2^32");
     return HF_ERR_SHAPE;
   }
   return HF_OK;

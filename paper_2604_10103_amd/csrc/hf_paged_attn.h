@@ -6,11 +6,16 @@
 // Items.  The grid is fixed by sizes that the host knows (packed rows, sequences, heads); which (sequence, rows, key head, part of the
 // keys) a workgroup works on follows from the lengths, which only the device knows: every wavefront derives it for itself from cu_new
 // and seq_lens, 64 sequences at a time, without exchange.  Keys count in tiles of 32.  A sequence whose rows see w tiles at most is cut
-// into S = ceil(w / C) parts of equal length, C = max(cmin, all tiles of all rows / target): about `target` parts of like size in all,
-// whatever the lengths are.  There are at most target + (row tiles) * heads_kv items, and at most 2 * target that are parts.
+// into ceil(w / C) parts of equal length, C = ceil(longest w / S).  S is the one of 64 candidates (one a lane) for which
+//     rounds of the chip (n S / slots, rounded up) * (longest w / S + start) + (S > 1 ? meet + join * S : 0)
+// is least, n the row tiles and key heads as if all were as long as the longest: a part costs its tiles and as much time as `start` tiles
+// besides, the meeting of a row's parts as much as meet + join * S.  Only S with n S <= target are looked at (and S = 1), so that there
+// are at most target + (row tiles) * heads_kv items, and at most 2 * target that are parts.
 //
 // Parts of a row meet in the workspace: each writes its sums (fp32) there, the last one to arrive adds them in the order of the parts.
 #pragma once
+
+#include <type_traits>
 
 #include "hf_paged.h"
 
@@ -19,12 +24,36 @@ namespace hf {
 constexpr int kKeyTile = 32;
 
 struct PagedSchedule {
-  int target, cmin, capacity;    // parts that the workspace holds
+  int target, capacity;          // capacity: parts that the workspace holds
+  int slots;                     // workgroups that the chip holds
+  float start, meet, join;       // in tiles
   unsigned long long* counters;  // [capacity] arrivals at a row tile, indexed by its first part
   float* parts;                  // [capacity][BM][D], behind them [capacity][BM][2]: row maximum and sum
   unsigned long long tag;
   bool by_xcd;                   // consecutive items on one XCD (they read the same keys)
 };
+
+struct PagedLaunch {   // the kernels' only argument
+  PagedAttnArgs a;
+  PagedSchedule sc;
+};
+// The arguments, read anew: kept over a kernel's phases they fill the scalar registers, and the loop would fetch spilled ones lane by lane
+__device__ __forceinline__ PagedLaunch launch_arguments() {
+  typedef const __attribute__((address_space(4))) uint32_t* Words;
+  static_assert(sizeof(PagedLaunch) % 4 == 0, "words");
+  Words p = (Words)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  struct { uint32_t w[sizeof(PagedLaunch) / 4]; } words;
+#pragma unroll
+  for (size_t i = 0; i < sizeof(PagedLaunch) / 4; ++i) words.w[i] = p[i];
+  PagedLaunch r = __builtin_bit_cast(PagedLaunch, words);
+  const auto global = [](auto& at) {   // (of an argument as such the compiler would know)
+    at = (std::remove_reference_t<decltype(at)>)(__attribute__((address_space(1))) std::remove_pointer_t<std::remove_reference_t<decltype(at)>>*)reinterpret_cast<uintptr_t>(at);
+  };
+  global(r.a.Q); global(r.a.K_pages); global(r.a.V_pages); global(r.a.O); global(r.a.cu); global(r.a.lens); global(r.a.table); global(r.a.lse2);
+  global(r.sc.counters); global(r.sc.parts);
+  return r;
+}
 
 // the key tiles of some rows: 0 .. s1 - 1 (sink), then from s1 + skip on; n of them
 struct KeyTiles {
@@ -74,13 +103,30 @@ template <int BM> __device__ __forceinline__ bool find_item(const PagedAttnArgs&
       }
     }
   };
-  float units = 0.0f;
+  float units = 0.0f, longest = 1.0f;
   for (int s0 = 0; s0 < a.n_seqs; s0 += kWave) {
     look(s0 + lane);
     units += (float)T * (float)w;
+    longest = fmaxf(longest, (float)w);
   }
-  units = wave_sum(units);
-  const int C = max(sc.cmin, (int)ceilf(fminf(units * (float)a.heads_kv / (float)sc.target, 1e9f)));
+  int C = 0x3fffffff;
+  if (sc.capacity > 0) {
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+      units += __shfl_xor(units, o, kWave);
+      longest = fmaxf(longest, __shfl_xor(longest, o, kWave));
+    }
+    const float n = units / longest * (float)a.heads_kv;
+    const float S = lane < 32 ? (float)(lane + 1) : floorf(32.0f * __builtin_amdgcn_exp2f((float)(lane - 31) * (5.0f / 32.0f)));   // .. 1024
+    float cost = ceilf(n * S / (float)sc.slots) * (longest / S + sc.start) + (lane > 0 ? sc.meet + sc.join * S : 0.0f);
+    if (lane > 0 && (n * S > (float)sc.target || S > longest)) cost = INFINITY;
+    float best = cost;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) best = fminf(best, __shfl_xor(best, o, kWave));
+    const int at = __ffsll(__ballot(cost == best)) - 1;
+    const float s_best = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(S), at));
+    if (at > 0) C = __builtin_amdgcn_readfirstlane((int)ceilf(longest / s_best));
+  }
   if (sc.by_xcd) {   // workgroup ids go round the XCDs: each takes one contiguous eighth of the items
     int total = 0;
     for (int s0 = 0; s0 < a.n_seqs; s0 += kWave) {
@@ -89,7 +135,7 @@ template <int BM> __device__ __forceinline__ bool find_item(const PagedAttnArgs&
     }
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) total += __shfl_xor(total, o, kWave);
-    const int per = (total + 7) / 8, slot = item >> 3;
+    const int per = (__builtin_amdgcn_readfirstlane(total) + 7) / 8, slot = item >> 3;
     if (slot >= per) return false;
     item = (item & 7) * per + slot;
   }
@@ -190,8 +236,6 @@ __device__ __forceinline__ void finish_item(const PagedAttnArgs& a, const PagedS
   constexpr int TPR = D / 8, PER = NT / TPR, PASS = (BM + PER - 1) / PER;
   const int tid = threadIdx.x, f = 8 * (tid % TPR), r0 = tid / TPR, group = a.heads / a.heads_kv;
   typedef unsigned long long u64;
-  float* const part_rows = sc.parts;
-  float* const part_stats = sc.parts + (size_t)sc.capacity * BM * D;
   __syncthreads();
   auto meet = [&](int row, float* acc, float& M, float& L) {   // the groups' parts of a row
     float mu[KS], lu[KS];
@@ -250,14 +294,14 @@ __device__ __forceinline__ void finish_item(const PagedAttnArgs& a, const PagedS
     }
     return;
   }
-  // ---- a part: its sums go past the caches of this XCD, each store acknowledged before the arrival
-  auto store2 = [](float* p, float x, float y) {
-    __hip_atomic_store(reinterpret_cast<u64*>(p), (u64)__float_as_uint(x) | ((u64)__float_as_uint(y) << 32), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  };
-  auto load2 = [](const float* p) {
-    const u64 v = __hip_atomic_load(const_cast<u64*>(reinterpret_cast<const u64*>(p)), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
-  };
+  // ---- a part: its sums go past the caches of this XCD (sc1), each store acknowledged before the arrival
+  constexpr int kSc1 = 16;
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  const __amdgpu_buffer_rsrc_t parts = __builtin_amdgcn_make_buffer_rsrc(sc.parts, 0, sc.capacity * (BM * (D + 2) * 4), 0x00020000);
+  const int stats_at_byte = sc.capacity * (BM * D * 4);
+  auto row_byte = [&](int slot, int row) { return (slot * BM + row) * (D * 4) + 4 * f; };
+  auto stat_byte = [&](int slot, int row) { return stats_at_byte + (slot * BM + row) * 8; };
   u64* const counter = sc.counters + it.counter;
   if (tid == 0) {   // a counter of another call counts from zero
     u64 seen = __hip_atomic_load(counter, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -270,10 +314,10 @@ __device__ __forceinline__ void finish_item(const PagedAttnArgs& a, const PagedS
     if (row >= it.rows) break;
     float acc[8], M, L;
     meet(row, acc, M, L);
-    float* to = part_rows + ((size_t)it.slot * BM + row) * D + f;
-#pragma unroll
-    for (int e = 0; e < 8; e += 2) store2(to + e, acc[e], acc[e + 1]);
-    if (f == 0) store2(part_stats + ((size_t)it.slot * BM + row) * 2, M, L);
+    const int to = row_byte(it.slot, row);
+    __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(acc[0]), __float_as_uint(acc[1]), __float_as_uint(acc[2]), __float_as_uint(acc[3])}, parts, to, 0, kSc1);
+    __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(acc[4]), __float_as_uint(acc[5]), __float_as_uint(acc[6]), __float_as_uint(acc[7])}, parts, to + 16, 0, kSc1);
+    if (f == 0) __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(M), __float_as_uint(L)}, parts, stat_byte(it.slot, row), 0, kSc1);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
@@ -285,38 +329,78 @@ __device__ __forceinline__ void finish_item(const PagedAttnArgs& a, const PagedS
   }
   __syncthreads();
   if (!*flag) return;
-  // ---- the last one: the parts of (row tile, key head) lie as many slots apart as the sequence has row tiles
+  // ---- the last one.  The parts of (row tile, key head) lie as many slots apart as the sequence has row tiles.  Few rows leave threads
+  // over: G sets of threads then take every G-th part each and meet in LDS, in their order
   const int tiles = (it.m * group + BM - 1) / BM;
+  int lanes_rows = 1;                                   // rows of a pass, a power of two
+  while (lanes_rows < it.rows && lanes_rows < PER) lanes_rows *= 2;
+  const int G = PER / lanes_rows, set = r0 / lanes_rows, rp = r0 % lanes_rows;
+  constexpr int LINE = 8 * TPR + 4;                     // floats of a row in LDS: sums, then (maximum, sum)
+  float* const meeting = const_cast<float*>(rows_at(0));
+  constexpr int U = 8;                                  // parts requested together
 #pragma unroll 1
-  for (int p = 0; p < PASS; ++p) {
-    const int row = r0 + p * PER;
-    if (row >= it.rows) break;
-    float M = -INFINITY;
-    const float* st = part_stats + ((size_t)it.counter * BM + row) * 2;
-    const size_t st_step = (size_t)tiles * BM * 2;
-#pragma unroll 8
-    for (int u = 0; u < it.parts; ++u) M = fmaxf(M, load2(st + u * st_step).x);
-    const float use = M == -INFINITY ? 0.0f : M;
-    float L = 0.0f, acc[8];
+  for (int p = 0; p < (it.rows + lanes_rows - 1) / lanes_rows; ++p) {
+    const int row = rp + p * lanes_rows, row_in = min(row, it.rows - 1);
+    float M = -INFINITY, L = 0.0f, acc[8];
     bool only = false;
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
-    const float* from = part_rows + ((size_t)it.counter * BM + row) * D + f;
-#pragma unroll 4
-    for (int u = 0; u < it.parts; ++u) {
-      const float2 s = load2(st + u * st_step);
-      const float wgt = __builtin_amdgcn_exp2f(s.x - use);
-      only = only || s.y == kOnlyInfinite;
-      L += s.y == kOnlyInfinite ? 0.0f : s.y * wgt;
+#pragma unroll 1
+    for (int u0 = set; u0 < it.parts; u0 += U * G) {
+      u32x2 st[U];
+      u32x4 v[U][2];
 #pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        const float2 v = load2(from + (size_t)u * tiles * BM * D + e);
-        acc[e] += v.x * wgt;
-        acc[e + 1] += v.y * wgt;
+      for (int i = 0; i < U; ++i) {
+        const int slot = it.counter + min(u0 + i * G, it.parts - 1) * tiles;
+        st[i] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(parts, stat_byte(slot, row_in), 0, kSc1));
+        v[i][0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(parts, row_byte(slot, row_in), 0, kSc1));
+        v[i][1] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(parts, row_byte(slot, row_in) + 16, 0, kSc1));
+      }
+      float top = M;
+#pragma unroll
+      for (int i = 0; i < U; ++i) top = fmaxf(top, u0 + i * G < it.parts ? __uint_as_float(st[i][0]) : -INFINITY);
+      const float use = top == -INFINITY ? 0.0f : top, w0 = __builtin_amdgcn_exp2f(M - use);
+      M = top;
+      L *= w0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] *= w0;
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        if (u0 + i * G >= it.parts) break;
+        const float wgt = __builtin_amdgcn_exp2f(__uint_as_float(st[i][0]) - use), l = __uint_as_float(st[i][1]);
+        only = only || l == kOnlyInfinite;
+        L += l == kOnlyInfinite ? 0.0f : l * wgt;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] += __uint_as_float(v[i][e >> 2][e & 3]) * wgt;
       }
     }
     if (only && M == -INFINITY && L == 0.0f) L = kOnlyInfinite;
-    write(row, acc, M, L);
+    if (G > 1) {   // (one pass then)
+      float* const line = meeting + r0 * LINE;
+#pragma unroll
+      for (int e = 0; e < 8; e += 4) *reinterpret_cast<float4*>(line + f + e) = make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
+      if (f == 0) *reinterpret_cast<float2*>(line + 8 * TPR) = make_float2(M, L);
+      __syncthreads();
+      if (set != 0) return;
+      const float* from = meeting + rp * LINE;
+      M = -INFINITY;
+      for (int g = 0; g < G; ++g) M = fmaxf(M, from[g * lanes_rows * LINE + 8 * TPR]);
+      const float use = M == -INFINITY ? 0.0f : M;
+      L = 0.0f;
+      only = false;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
+      for (int g = 0; g < G; ++g) {
+        const float* x = from + g * lanes_rows * LINE;
+        const float l = x[8 * TPR + 1], wgt = __builtin_amdgcn_exp2f(x[8 * TPR] - use);
+        only = only || l == kOnlyInfinite;
+        L += l == kOnlyInfinite ? 0.0f : l * wgt;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] += x[f + e] * wgt;
+      }
+      if (only && M == -INFINITY && L == 0.0f) L = kOnlyInfinite;
+    }
+    if (row < it.rows) write(row, acc, M, L);
   }
 }
 

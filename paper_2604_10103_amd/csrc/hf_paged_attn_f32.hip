@@ -10,6 +10,7 @@ namespace hf {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+#define HF_GLOBAL __attribute__((address_space(1)))   // (of an address that went from lane to lane the compiler would not know)
 
 namespace {
 
@@ -18,14 +19,18 @@ __device__ float zero_row_f32[128];
 __device__ __forceinline__ bool not_finite(float v) { return (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u; }
 
 template <int D, int NW, int KS>
-__global__ __launch_bounds__(64 * NW * KS, 1) void paged_attn_f32_kernel(const PagedAttnArgs a, const PagedSchedule sc) {
+__global__ __launch_bounds__(64 * NW * KS, 1) void paged_attn_f32_kernel(const PagedLaunch) {
   constexpr int BM = 32 * NW, NT = 64 * NW * KS, NC = D / 8, E = D / 32;   // 16-byte pieces of a key; features of a lane's piece of a value
   constexpr int SPAN = BM * (D + 4) + BM * 2;                              // a group's sums and statistics, in floats
   extern __shared__ __attribute__((aligned(16))) float sums[];
   typedef float piece __attribute__((ext_vector_type(E)));
 
   PagedItem it;
-  if (!find_item<BM>(a, sc, blockIdx.x, it)) return;
+  {
+    const PagedLaunch p = launch_arguments();
+    if (!find_item<BM>(p.a, p.sc, blockIdx.x, it)) return;
+  }
+  const PagedAttnArgs a = launch_arguments().a;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave_in_wg = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wave = wave_in_wg % NW, grp = wave_in_wg / NW;
@@ -71,9 +76,9 @@ __global__ __launch_bounds__(64 * NW * KS, 1) void paged_attn_f32_kernel(const P
     return (id * page_rows + head_row + (key - div_page(a, key) * a.page)) * D;
   };
   auto load_keys = [&](f32x4 (&k)[NC], int i, int id) {
-    const float* p = (id >= 0 ? static_cast<const float*>(a.K_pages) + offset_of(i, id) : zero_row_f32) + 4 * h;
+    const uintptr_t p = reinterpret_cast<uintptr_t>((id >= 0 ? static_cast<const float*>(a.K_pages) + offset_of(i, id) : zero_row_f32) + 4 * h);
 #pragma unroll
-    for (int c = 0; c < NC; ++c) k[c] = *reinterpret_cast<const f32x4*>(p + 8 * c);
+    for (int c = 0; c < NC; ++c) k[c] = *(const HF_GLOBAL f32x4*)(p + 32 * c);
   };
   int id = -1, id_next = -1;
   f32x4 kf[NC];
@@ -84,18 +89,17 @@ __global__ __launch_bounds__(64 * NW * KS, 1) void paged_attn_f32_kernel(const P
   }
   bool odd = false;   // values that are not finite lie next to rows that do not see them: they were left out (uniform)
 
+#pragma unroll 1
   for (int i = 0; i < count; ++i) {
     const int start = start_of(i);
     const uint32_t exists = (uint32_t)__ballot(id >= 0);
     const float* const v_row = id >= 0 ? static_cast<const float*>(a.V_pages) + offset_of(i, id) : zero_row_f32;
-    auto row_of = [&](int key) {   // of the tile
-      return reinterpret_cast<const float*>(__shfl((unsigned long long)reinterpret_cast<uintptr_t>(v_row), key, kWave));
-    };
+    auto row_of = [&](int key) { return (uintptr_t)__shfl((unsigned long long)reinterpret_cast<uintptr_t>(v_row), key, kWave); };   // of the tile
     const int id_after = page_of(i + 2);
     if (some_of(start)) {
       piece vf[16];
 #pragma unroll
-      for (int r = 0; r < 16; ++r) vf[r] = *reinterpret_cast<const piece*>(row_of(8 * (r >> 2) + 4 * h + (r & 3)) + E * l32);
+      for (int r = 0; r < 16; ++r) vf[r] = *(const HF_GLOBAL piece*)(row_of(8 * (r >> 2) + 4 * h + (r & 3)) + 4 * E * l32);
       f32x16 sacc;
 #pragma unroll
       for (int r = 0; r < 16; ++r) sacc[r] = 0.0f;
@@ -186,7 +190,7 @@ __global__ __launch_bounds__(64 * NW * KS, 1) void paged_attn_f32_kernel(const P
           const piece w = *reinterpret_cast<const piece*>(vr + E * (8 * (r >> 2) + 4 * h + (r & 3)));
 #pragma unroll
           for (int e = 0; e < E; ++e)
-            if (sees && not_finite(w[e])) o[e][r] += positive ? w[e] : __builtin_nanf("");
+            o[e][r] += sees && not_finite(w[e]) ? (positive ? w[e] : __builtin_nanf("")) : 0.0f;
         }
       }
     }
@@ -203,7 +207,8 @@ __global__ __launch_bounds__(64 * NW * KS, 1) void paged_attn_f32_kernel(const P
     *reinterpret_cast<piece*>(row + E * (8 * (r >> 2) + 4 * h + (r & 3))) = y;
   }
   if (h == 0) *reinterpret_cast<float2*>(sums + grp * SPAN + BM * (D + 4) + 2 * (32 * wave + l32)) = make_float2(m_ref, l_run);
-  finish_item<float, D, BM, KS, NT>(a, sc, it, [&](int u) { return sums + u * SPAN; }, [&](int u) { return sums + u * SPAN + BM * (D + 4); },
+  const PagedLaunch p = launch_arguments();
+  finish_item<float, D, BM, KS, NT>(p.a, p.sc, it, [&](int u) { return sums + u * SPAN; }, [&](int u) { return sums + u * SPAN + BM * (D + 4); },
                                     reinterpret_cast<int*>(sums + KS * SPAN));
 }
 
@@ -212,7 +217,7 @@ template <int D, int NW, int KS> int launch(const PagedAttnArgs& a, const PagedS
   static LdsGrant grant;
   const int rc = grant_lds(grant, reinterpret_cast<const void*>(&paged_attn_f32_kernel<D, NW, KS>), kLds, "hf_paged_attn_fwd");
   if (rc != HF_OK) return rc;
-  hipLaunchKernelGGL((paged_attn_f32_kernel<D, NW, KS>), dim3(items), dim3(64 * NW * KS), kLds, s, a, sc);
+  hipLaunchKernelGGL((paged_attn_f32_kernel<D, NW, KS>), dim3(items), dim3(64 * NW * KS), kLds, s, PagedLaunch{a, sc});
   return check_launch("hf_paged_attn_fwd");
 }
 
