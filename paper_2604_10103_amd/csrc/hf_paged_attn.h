@@ -6,11 +6,11 @@
 // Items.  The grid is fixed by sizes that the host knows (packed rows, sequences, heads); which (sequence, rows, key head, part of the
 // keys) a workgroup works on follows from the lengths, which only the device knows: every wavefront derives it for itself from cu_new
 // and seq_lens, 64 sequences at a time, without exchange.  Keys count in tiles of 32.  A sequence whose rows see w tiles at most is cut
-// into ceil(w / C) parts of equal length, C = ceil(longest w / S).  S is the one of 64 candidates (one a lane) for which
-//     rounds of the chip (n S / slots, rounded up) * (longest w / S + start) + (S > 1 ? meet + join * S : 0)
-// is least, n the row tiles and key heads as if all were as long as the longest: a part costs its tiles and as much time as `start` tiles
-// besides, the meeting of a row's parts as much as meet + join * S.  Only S with n S <= target are looked at (and S = 1), so that there
-// are at most target + (row tiles) * heads_kv items, and at most 2 * target that are parts.
+// into ceil(w / C) parts of equal length, C = ceil(longest w / S).  S is the one of 64 candidates (one a lane) for which a model of the
+// launch is least: with n = the work in row tiles as long as the longest, x = n S / compute units,
+//     rounds(x) * (longest w / S * tile + start) + (S > 1 ? meet + join * S : 0)      microseconds,
+// rounds(x) = x rounded up where all rows see as much, else x + 3/4 (workgroups take what is next as they become free).  Only S with
+// n S <= target are looked at (and S = 1), so that there are at most target + (row tiles) * heads_kv items, of which 2 * target are parts.
 //
 // Parts of a row meet in the workspace: each writes its sums (fp32) there, the last one to arrive adds them in the order of the parts.
 #pragma once
@@ -22,11 +22,12 @@
 namespace hf {
 
 constexpr int kKeyTile = 32;
+constexpr float kComputeUnits = 256;
 
 struct PagedSchedule {
   int target, capacity;          // capacity: parts that the workspace holds
-  int slots;                     // workgroups that the chip holds
-  float start, meet, join;       // in tiles
+  float tile, tile_alone;        // microseconds a tile takes where the chip is full, and at least
+  float start, meet, join;
   unsigned long long* counters;  // [capacity] arrivals at a row tile, indexed by its first part
   float* parts;                  // [capacity][BM][D], behind them [capacity][BM][2]: row maximum and sum
   unsigned long long tag;
@@ -87,9 +88,9 @@ struct PagedItem {
 template <int BM> __device__ __forceinline__ bool find_item(const PagedAttnArgs& a, const PagedSchedule& sc, int item, PagedItem& it) {
   const int lane = threadIdx.x & 63, group = a.heads / a.heads_kv;
   const int most = a.max_pages * a.page;
-  int begin = 0, m = 0, len = 0, T = 0, w = 0;
+  int begin = 0, m = 0, len = 0, T = 0, w = 0, w_least = 0;   // T row tiles that see w_least .. w key tiles
   auto look = [&](int s) {
-    begin = m = len = T = w = 0;
+    begin = m = len = T = w = w_least = 0;
     if (s < a.n_seqs) {
       begin = min(max(a.cu[s], 0), a.n_q);
       m = min(max(a.cu[s + 1], begin), a.n_q) - begin;
@@ -100,26 +101,33 @@ template <int BM> __device__ __forceinline__ bool find_item(const PagedAttnArgs&
         const KeyTiles x = key_tiles(a, m, len, held, 0, min(m, (BM - 1) / group + 1) - 1);
         const KeyTiles y = key_tiles(a, m, len, held, (T - 1) * BM / group, m - 1);
         w = max(1, max(x.n, y.n));
+        w_least = max(1, min(x.n, y.n));
       }
     }
   };
-  float units = 0.0f, longest = 1.0f;
+  float most_units = 0.0f, units = 0.0f, rows = 0.0f, longest = 1.0f;
   for (int s0 = 0; s0 < a.n_seqs; s0 += kWave) {
     look(s0 + lane);
-    units += (float)T * (float)w;
+    most_units += (float)T * (float)w;
+    units += (float)T * 0.5f * (float)(w + w_least);
+    rows += (float)T;
     longest = fmaxf(longest, (float)w);
   }
   int C = 0x3fffffff;
   if (sc.capacity > 0) {
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) {
+      most_units += __shfl_xor(most_units, o, kWave);
       units += __shfl_xor(units, o, kWave);
+      rows += __shfl_xor(rows, o, kWave);
       longest = fmaxf(longest, __shfl_xor(longest, o, kWave));
     }
     const float n = units / longest * (float)a.heads_kv;
     const float S = lane < 32 ? (float)(lane + 1) : floorf(32.0f * __builtin_amdgcn_exp2f((float)(lane - 31) * (5.0f / 32.0f)));   // .. 1024
-    float cost = ceilf(n * S / (float)sc.slots) * (longest / S + sc.start) + (lane > 0 ? sc.meet + sc.join * S : 0.0f);
-    if (lane > 0 && (n * S > (float)sc.target || S > longest)) cost = INFINITY;
+    const float x = n * S * (1.0f / kComputeUnits);
+    const float rounds = x <= 1.0f ? 1.0f : (units > 0.98f * longest * rows ? ceilf(x) : x + 0.75f);
+    float cost = rounds * (longest / S * fmaxf(sc.tile_alone, sc.tile * fminf(x, 1.0f)) + sc.start) + (lane > 0 ? sc.meet + sc.join * S : 0.0f);
+    if (lane > 0 && (most_units / longest * (float)a.heads_kv * S > (float)sc.target || S > longest)) cost = INFINITY;
     float best = cost;
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) best = fminf(best, __shfl_xor(best, o, kWave));
@@ -127,22 +135,33 @@ template <int BM> __device__ __forceinline__ bool find_item(const PagedAttnArgs&
     const float s_best = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(S), at));
     if (at > 0) C = __builtin_amdgcn_readfirstlane((int)ceilf(longest / s_best));
   }
-  if (sc.by_xcd) {   // workgroup ids go round the XCDs: each takes one contiguous eighth of the items
-    int total = 0;
-    for (int s0 = 0; s0 < a.n_seqs; s0 += kWave) {
-      if (a.n_seqs > kWave) look(s0 + lane);
-      total += T * ((w + C - 1) / C) * a.heads_kv;
-    }
+  // items of one key head: the item's head, and its place among them
+  int each = 0, split_each = 0;
+  for (int s0 = 0; s0 < a.n_seqs; s0 += kWave) {
+    if (a.n_seqs > kWave) look(s0 + lane);
+    const int S = (w + C - 1) / C;
+    each += T * S;
+    split_each += S > 1 ? T * S : 0;
+  }
 #pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) total += __shfl_xor(total, o, kWave);
-    const int per = (__builtin_amdgcn_readfirstlane(total) + 7) / 8, slot = item >> 3;
+  for (int o = 1; o < kWave; o <<= 1) {
+    each += __shfl_xor(each, o, kWave);
+    split_each += __shfl_xor(split_each, o, kWave);
+  }
+  each = __builtin_amdgcn_readfirstlane(each);
+  split_each = __builtin_amdgcn_readfirstlane(split_each);
+  if (sc.by_xcd) {   // workgroup ids go round the XCDs: each takes one contiguous eighth of the items
+    const int per = (each * a.heads_kv + 7) / 8, slot = item >> 3;
     if (slot >= per) return false;
     item = (item & 7) * per + slot;
   }
+  if (item >= each * a.heads_kv || split_each * a.heads_kv > sc.capacity) return false;   // (the latter cannot be, see above)
+  it.head_kv = item / each;
+  item -= it.head_kv * each;
   int before = 0, split_before = 0;   // items and parts of the sequences before
   for (int s0 = 0; s0 < a.n_seqs; s0 += kWave) {
     if (a.n_seqs > kWave) look(s0 + lane);
-    const int S = (w + C - 1) / C, mine = T * S * a.heads_kv;
+    const int S = (w + C - 1) / C, mine = T * S;
     int upto = mine, split_upto = S > 1 ? mine : 0;
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) {
@@ -160,14 +179,12 @@ template <int BM> __device__ __forceinline__ bool find_item(const PagedAttnArgs&
       it.held = min(it.len, most);
       it.parts = of(S);
       const int tiles = of(T), own = of(mine), idx = item - (before + of(upto) - own);
-      const int slot0 = split_before + of(split_upto) - own;   // (meant where there are parts)
-      // within a sequence: key head, part, then rows, the last ones (which see most) first
-      const int x = idx / tiles, r = tiles - 1 - (idx - x * tiles);
-      it.head_kv = x / it.parts;
-      it.part = x - it.head_kv * it.parts;
+      const int slot0 = it.head_kv * split_each + split_before + of(split_upto) - own;   // (meant where there are parts)
+      // within a sequence: part, then rows, the last ones (which see most) first
+      it.part = idx / tiles;
+      const int back = idx - it.part * tiles, r = tiles - 1 - back;
       it.slot = slot0 + idx;
-      it.counter = slot0 + it.head_kv * it.parts * tiles + idx - x * tiles;
-      if (it.parts > 1 && slot0 + own > sc.capacity) return false;   // (cannot be, see above)
+      it.counter = slot0 + back;
       it.first = r * BM;
       it.rows = min(BM, it.m * group - it.first);
       it.keys = key_tiles(a, it.m, it.len, it.held, it.first / group, (it.first + it.rows - 1) / group);
@@ -337,71 +354,103 @@ __device__ __forceinline__ void finish_item(const PagedAttnArgs& a, const PagedS
   const int G = PER / lanes_rows, set = r0 / lanes_rows, rp = r0 % lanes_rows;
   constexpr int LINE = 8 * TPR + 4;                     // floats of a row in LDS: sums, then (maximum, sum)
   float* const meeting = const_cast<float*>(rows_at(0));
-  constexpr int U = 8;                                  // parts requested together
-#pragma unroll 1
-  for (int p = 0; p < (it.rows + lanes_rows - 1) / lanes_rows; ++p) {
-    const int row = rp + p * lanes_rows, row_in = min(row, it.rows - 1);
-    float M = -INFINITY, L = 0.0f, acc[8];
-    bool only = false;
+  const int passes = (it.rows + lanes_rows - 1) / lanes_rows;
+  // R rows (of passes p ..) times U parts are requested together: few parts of many rows, or many parts of few
+  auto join = [&](auto r_of, auto u_of, int p, float (&M)[decltype(r_of)::value], float (&L)[decltype(r_of)::value], float (&acc)[decltype(r_of)::value][8]) {
+    constexpr int R = decltype(r_of)::value, U = decltype(u_of)::value;
+    bool only[R];
+    int row[R];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
+    for (int r = 0; r < R; ++r) {
+      M[r] = -INFINITY;
+      L[r] = 0.0f;
+      only[r] = false;
+      row[r] = min(rp + (p + r) * lanes_rows, it.rows - 1);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[r][e] = 0.0f;
+    }
 #pragma unroll 1
     for (int u0 = set; u0 < it.parts; u0 += U * G) {
-      u32x2 st[U];
-      u32x4 v[U][2];
+      u32x2 st[R][U];
+      u32x4 v[R][U][2];
 #pragma unroll
-      for (int i = 0; i < U; ++i) {
-        const int slot = it.counter + min(u0 + i * G, it.parts - 1) * tiles;
-        st[i] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(parts, stat_byte(slot, row_in), 0, kSc1));
-        v[i][0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(parts, row_byte(slot, row_in), 0, kSc1));
-        v[i][1] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(parts, row_byte(slot, row_in) + 16, 0, kSc1));
-      }
-      float top = M;
+      for (int i = 0; i < U; ++i)
 #pragma unroll
-      for (int i = 0; i < U; ++i) top = fmaxf(top, u0 + i * G < it.parts ? __uint_as_float(st[i][0]) : -INFINITY);
-      const float use = top == -INFINITY ? 0.0f : top, w0 = __builtin_amdgcn_exp2f(M - use);
-      M = top;
-      L *= w0;
+        for (int r = 0; r < R; ++r) {
+          const int slot = it.counter + min(u0 + i * G, it.parts - 1) * tiles;
+          st[r][i] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(parts, stat_byte(slot, row[r]), 0, kSc1));
+          v[r][i][0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(parts, row_byte(slot, row[r]), 0, kSc1));
+          v[r][i][1] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(parts, row_byte(slot, row[r]) + 16, 0, kSc1));
+        }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] *= w0;
+      for (int r = 0; r < R; ++r) {
+        float top = M[r];
 #pragma unroll
-      for (int i = 0; i < U; ++i) {
-        if (u0 + i * G >= it.parts) break;
-        const float wgt = __builtin_amdgcn_exp2f(__uint_as_float(st[i][0]) - use), l = __uint_as_float(st[i][1]);
-        only = only || l == kOnlyInfinite;
-        L += l == kOnlyInfinite ? 0.0f : l * wgt;
+        for (int i = 0; i < U; ++i) top = fmaxf(top, u0 + i * G < it.parts ? __uint_as_float(st[r][i][0]) : -INFINITY);
+        const float use = top == -INFINITY ? 0.0f : top, w0 = __builtin_amdgcn_exp2f(M[r] - use);
+        M[r] = top;
+        L[r] *= w0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] += __uint_as_float(v[i][e >> 2][e & 3]) * wgt;
+        for (int e = 0; e < 8; ++e) acc[r][e] *= w0;
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          if (u0 + i * G >= it.parts) break;
+          const float wgt = __builtin_amdgcn_exp2f(__uint_as_float(st[r][i][0]) - use), l = __uint_as_float(st[r][i][1]);
+          only[r] = only[r] || l == kOnlyInfinite;
+          L[r] += l == kOnlyInfinite ? 0.0f : l * wgt;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) acc[r][e] += __uint_as_float(v[r][i][e >> 2][e & 3]) * wgt;
+        }
       }
     }
-    if (only && M == -INFINITY && L == 0.0f) L = kOnlyInfinite;
-    if (G > 1) {   // (one pass then)
-      float* const line = meeting + r0 * LINE;
 #pragma unroll
-      for (int e = 0; e < 8; e += 4) *reinterpret_cast<float4*>(line + f + e) = make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
-      if (f == 0) *reinterpret_cast<float2*>(line + 8 * TPR) = make_float2(M, L);
-      __syncthreads();
-      if (set != 0) return;
-      const float* from = meeting + rp * LINE;
-      M = -INFINITY;
-      for (int g = 0; g < G; ++g) M = fmaxf(M, from[g * lanes_rows * LINE + 8 * TPR]);
-      const float use = M == -INFINITY ? 0.0f : M;
-      L = 0.0f;
-      only = false;
+    for (int r = 0; r < R; ++r)
+      if (only[r] && M[r] == -INFINITY && L[r] == 0.0f) L[r] = kOnlyInfinite;
+  };
+  if (G == 1) {
+    auto all_rows = [&](auto r_of, auto u_of) {
+      constexpr int R = decltype(r_of)::value;
+#pragma unroll 1
+      for (int p = 0; p < passes; p += R) {
+        float M[R], L[R], acc[R][8];
+        join(r_of, u_of, p, M, L, acc);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
-      for (int g = 0; g < G; ++g) {
-        const float* x = from + g * lanes_rows * LINE;
-        const float l = x[8 * TPR + 1], wgt = __builtin_amdgcn_exp2f(x[8 * TPR] - use);
-        only = only || l == kOnlyInfinite;
-        L += l == kOnlyInfinite ? 0.0f : l * wgt;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] += x[f + e] * wgt;
+        for (int r = 0; r < R; ++r) {
+          const int row = rp + (p + r) * lanes_rows;
+          if (row < it.rows) write(row, acc[r], M[r], L[r]);
+        }
       }
-      if (only && M == -INFINITY && L == 0.0f) L = kOnlyInfinite;
-    }
-    if (row < it.rows) write(row, acc, M, L);
+    };
+    if (it.parts <= 2) all_rows(std::integral_constant<int, 4>{}, std::integral_constant<int, 2>{});
+    else if (it.parts <= 4) all_rows(std::integral_constant<int, 2>{}, std::integral_constant<int, 4>{});
+    else all_rows(std::integral_constant<int, 1>{}, std::integral_constant<int, 8>{});
+    return;
   }
+  float Ms[1], Ls[1], sum[1][8];
+  join(std::integral_constant<int, 1>{}, std::integral_constant<int, 8>{}, 0, Ms, Ls, sum);
+  float* const line = meeting + r0 * LINE;
+#pragma unroll
+  for (int e = 0; e < 8; e += 4) *reinterpret_cast<float4*>(line + f + e) = make_float4(sum[0][e], sum[0][e + 1], sum[0][e + 2], sum[0][e + 3]);
+  if (f == 0) *reinterpret_cast<float2*>(line + 8 * TPR) = make_float2(Ms[0], Ls[0]);
+  __syncthreads();
+  if (set != 0 || rp >= it.rows) return;
+  const float* from = meeting + rp * LINE;
+  float M = -INFINITY, L = 0.0f, acc[8];
+  for (int g = 0; g < G; ++g) M = fmaxf(M, from[g * lanes_rows * LINE + 8 * TPR]);
+  const float use = M == -INFINITY ? 0.0f : M;
+  bool only = false;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
+  for (int g = 0; g < G; ++g) {
+    const float* x = from + g * lanes_rows * LINE;
+    const float l = x[8 * TPR + 1], wgt = __builtin_amdgcn_exp2f(x[8 * TPR] - use);
+    only = only || l == kOnlyInfinite;
+    L += l == kOnlyInfinite ? 0.0f : l * wgt;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] += x[f + e] * wgt;
+  }
+  if (only && M == -INFINITY && L == 0.0f) L = kOnlyInfinite;
+  write(rp, acc, M, L);
 }
 
 }  // namespace hf

@@ -465,18 +465,25 @@ struct Plan {
   PagedSchedule sc;
 };
 
-constexpr int kComputeUnits = 256;
-
 Plan plan_of(const hf_paged& c, int n_q) {
   const int group = c.heads / c.heads_kv;
   Plan p = {};
   // a workgroup of 128 rows where a sequence has more than 32 on the average
   p.rows = (long long)n_q * group > 32ll * c.n_seqs ? 128 : 32;
-  p.sc.slots = (p.rows == 128 ? 2 : 1) * kComputeUnits;
-  p.sc.target = 4 * kComputeUnits;
-  p.sc.start = p.rows == 128 ? 6.0f : 8.0f;
-  p.sc.meet = p.rows == 128 ? 6.0f : 6.0f;
-  p.sc.join = p.rows == 128 ? 1.0f : 0.25f;
+  if (p.rows == 128) {
+    p.sc.target = 1536;
+    p.sc.tile = p.sc.tile_alone = 0.535f;
+    p.sc.start = 3.0f;
+    p.sc.meet = 6.0f;
+    p.sc.join = 0.5f;
+  } else {
+    p.sc.target = 1024;
+    p.sc.tile = 0.8f;
+    p.sc.tile_alone = 0.22f;
+    p.sc.start = 4.0f;
+    p.sc.meet = 5.0f;
+    p.sc.join = 0.1f;
+  }
   p.sc.by_xcd = p.rows == 128;
   const long long tiles = ((long long)n_q * group / p.rows + (n_q < c.n_seqs ? n_q : c.n_seqs)) * c.heads_kv;   // (at most)
   const long long key_tiles = ((long long)c.max_pages * c.page_tokens + kKeyTile - 1) / kKeyTile;
