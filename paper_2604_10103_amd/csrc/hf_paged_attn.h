@@ -3,14 +3,21 @@
 // Rows.  The query heads of a group read the same keys, so a sequence's rows are numbered token by token, head by head of the group:
 // row x of (sequence, key head h) is token x / group, query head h * group + x % group.  A workgroup takes BM of them.
 //
-// Items.  The grid is fixed by sizes that the host knows (packed rows, sequences, heads); which (sequence, rows, key head, part of the
-// keys) a workgroup works on follows from the lengths, which only the device knows: every wavefront derives it for itself from cu_new
-// and seq_lens, 64 sequences at a time, without exchange.  Keys count in tiles of 32.  A sequence whose rows see w tiles at most is cut
-// into ceil(w / C) parts of equal length, C = ceil(longest w / S).  S is the one of 64 candidates (one a lane) for which a model of the
-// launch is least: with n = the work in row tiles as long as the longest, x = n S / compute units,
-//     rounds(x) * (longest w / S * tile + start) + (S > 1 ? meet + join * S : 0)      microseconds,
-// rounds(x) = x rounded up where all rows see as much, else x + 3/4 (workgroups take what is next as they become free).  Only S with
-// n S <= target are looked at (and S = 1), so that there are at most target + (row tiles) * heads_kv items, of which 2 * target are parts.
+// Work.  The grid is fixed by what the host knows; what a workgroup does follows from the lengths, which only the device knows: every
+// wavefront derives it for itself from cu_new and seq_lens, 64 sequences at a time, without exchange.  Keys count in tiles of 32.
+//
+//   pieces  A sequence whose rows see w tiles at most is cut into ceil(w / C) parts of equal length, C = ceil(longest w / S); a workgroup
+//           takes a (key head, sequence, part, rows).  S is the best of 64 candidates, one a lane, by a model of the launch: with n = the
+//           work in row tiles as long as the longest and x = n S / compute units,
+//               rounds(x) (longest w / S * tile + start) + (S > 1 ? meet + join S : 0)  microseconds,
+//           rounds(x) = x rounded up where all rows see as much, else x + 3/4.  Only S with n S <= groups are looked at, and S = 1.
+//   shares  (few rows, where no two workgroups read the same keys) All row tiles of all key heads lie on one line, each as long as its
+//           key tiles (between a sequence's first and last row tile they are taken to grow evenly) and `lead` more for what its start
+//           costs; each of `groups` workgroups gets an equal share of the line.  A share's end that falls near a row tile's ends moves
+//           there.  So a workgroup has whole row tiles and at most two parts.
+// Where workgroups of 32 rows have work for more than one round, shares are taken if the model expects them to be faster: 64 single
+// tokens over 500 to 8191 keys 225 us, in pieces 266.  Rows of chunks read the same keys at the same time when they lie in pieces, and
+// find them in the L2; in shares they do not (4680 rows over 9360 keys: 314 us in pieces, 354 in shares).
 //
 // Parts of a row meet in the workspace: each writes its sums (fp32) there, the last one to arrive adds them in the order of the parts.
 #pragma once
@@ -22,16 +29,16 @@
 namespace hf {
 
 constexpr int kKeyTile = 32;
-constexpr float kComputeUnits = 256;
 
 struct PagedSchedule {
-  int target, capacity;          // capacity: parts that the workspace holds
+  int groups;                    // workgroups that may be parts of a row tile's work (32 rows: the grid, if there is work for so many)
+  int lead;
+  bool meets;                    // there is a workspace: 2 groups parts, and as many counters
   float tile, tile_alone;        // microseconds a tile takes where the chip is full, and at least
   float start, meet, join;
-  unsigned long long* counters;  // [capacity] arrivals at a row tile, indexed by its first part
-  float* parts;                  // [capacity][BM][D], behind them [capacity][BM][2]: row maximum and sum
+  unsigned long long* counters;  // [2 groups] arrivals at a row tile
+  float* parts;                  // [2 groups][BM][D], behind them [2 groups][BM][2]: row maximum and sum
   unsigned long long tag;
-  bool by_xcd;                   // consecutive items on one XCD (they read the same keys)
 };
 
 struct PagedLaunch {   // the kernels' only argument
@@ -54,6 +61,13 @@ __device__ __forceinline__ PagedLaunch launch_arguments() {
   global(r.a.Q); global(r.a.K_pages); global(r.a.V_pages); global(r.a.O); global(r.a.cu); global(r.a.lens); global(r.a.table); global(r.a.lse2);
   global(r.sc.counters); global(r.sc.parts);
   return r;
+}
+
+// the thread's number, as if unknown before: what follows from it is formed anew in every phase instead of being kept over the others
+__device__ __forceinline__ int thread_id() {
+  int t = threadIdx.x;
+  asm volatile("" : "+v"(t));
+  return t;
 }
 
 // the key tiles of some rows: 0 .. s1 - 1 (sink), then from s1 + skip on; n of them
@@ -80,120 +94,265 @@ __device__ __forceinline__ KeyTiles key_tiles(const PagedAttnArgs& a, int m, int
 struct PagedItem {
   int seq, begin, m, len, held;   // first packed row, new tokens, length, tokens that can lie in the cache
   int head_kv, first, rows;       // rows first .. first + rows - 1 of the sequence
-  int part, parts, slot, counter; // which part of how many; its place in the workspace, and its row tile's counter
+  int part, parts, counter;       // which part of how many, and the row tile's counter
+  int slot0, slot1, slot_step;    // where the first part, the second, and the others behind it lie in the workspace
   int t0, t1;                     // its key tiles
   KeyTiles keys;
+  __device__ __forceinline__ int slot(int u) const { return u == 0 ? slot0 : slot1 + (u - 1) * slot_step; }
 };
 
-template <int BM> __device__ __forceinline__ bool find_item(const PagedAttnArgs& a, const PagedSchedule& sc, int item, PagedItem& it) {
-  const int lane = threadIdx.x & 63, group = a.heads / a.heads_kv;
-  const int most = a.max_pages * a.page;
-  int begin = 0, m = 0, len = 0, T = 0, w = 0, w_least = 0;   // T row tiles that see w_least .. w key tiles
-  auto look = [&](int s) {
-    begin = m = len = T = w = w_least = 0;
-    if (s < a.n_seqs) {
-      begin = min(max(a.cu[s], 0), a.n_q);
-      m = min(max(a.cu[s + 1], begin), a.n_q) - begin;
-      len = max(a.lens[s], 0);
-      if (m > 0) {
-        T = (m * group + BM - 1) / BM;
-        const int held = min(len, most);
-        const KeyTiles x = key_tiles(a, m, len, held, 0, min(m, (BM - 1) / group + 1) - 1);
-        const KeyTiles y = key_tiles(a, m, len, held, (T - 1) * BM / group, m - 1);
-        w = max(1, max(x.n, y.n));
-        w_least = max(1, min(x.n, y.n));
-      }
-    }
+// ---- over a wavefront, by data-parallel moves within its registers: inclusive sums, and totals that every lane (and the scalar unit) has
+__device__ __forceinline__ int scan_sum(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);   // the lane 1, 2, 4, 8 before, within 16
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // lanes 15 and 47 to the 16 behind
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // lane 31 to the 32 behind
+  return v;
+}
+__device__ __forceinline__ int total_sum(int v) { return __builtin_amdgcn_readlane(scan_sum(v), 63); }
+template <class F> __device__ __forceinline__ float total_of(float v, float neutral, F f) {
+  auto moved = [&](auto ctrl, auto rows, float x) {
+    return __uint_as_float(__builtin_amdgcn_update_dpp(__float_as_uint(neutral), __float_as_uint(x), decltype(ctrl)::value, decltype(rows)::value, 0xf, false));
   };
-  float most_units = 0.0f, units = 0.0f, rows = 0.0f, longest = 1.0f;
-  for (int s0 = 0; s0 < a.n_seqs; s0 += kWave) {
-    look(s0 + lane);
-    most_units += (float)T * (float)w;
-    units += (float)T * 0.5f * (float)(w + w_least);
-    rows += (float)T;
-    longest = fmaxf(longest, (float)w);
+  using std::integral_constant;
+  v = f(v, moved(integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{}, v));
+  v = f(v, moved(integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{}, v));
+  v = f(v, moved(integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{}, v));
+  v = f(v, moved(integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{}, v));
+  v = f(v, moved(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{}, v));
+  v = f(v, moved(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{}, v));
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
+}
+
+// a lane's sequence: T row tiles, of which the first sees v0 key tiles (at least 1) and the last v1
+struct SeqWork {
+  int begin, m, len, T, v0, v1;
+};
+template <int BM> __device__ __forceinline__ SeqWork seq_work(const PagedAttnArgs& a, int s) {
+  SeqWork q = {0, 0, 0, 0, 1, 1};
+  if (s >= a.n_seqs) return q;
+  const int group = a.heads / a.heads_kv;
+  q.begin = min(max(a.cu[s], 0), a.n_q);
+  q.m = min(max(a.cu[s + 1], q.begin), a.n_q) - q.begin;
+  q.len = max(a.lens[s], 0);
+  if (q.m > 0) {
+    q.T = (q.m * group + BM - 1) / BM;
+    const int held = min(q.len, a.max_pages * a.page);
+    q.v0 = max(1, key_tiles(a, q.m, q.len, held, 0, min(q.m, (BM - 1) / group + 1) - 1).n);
+    q.v1 = max(1, key_tiles(a, q.m, q.len, held, (q.T - 1) * BM / group, q.m - 1).n);
   }
-  int C = 0x3fffffff;
-  if (sc.capacity > 0) {
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-      most_units += __shfl_xor(most_units, o, kWave);
-      units += __shfl_xor(units, o, kWave);
-      rows += __shfl_xor(rows, o, kWave);
-      longest = fmaxf(longest, __shfl_xor(longest, o, kWave));
-    }
-    const float n = units / longest * (float)a.heads_kv;
+  return q;
+}
+
+// how the work is shared out (uniform)
+struct PagedWork {
+  bool shares;
+  int C, each, split_each;   // pieces: tiles of a part at most, pieces of a key head, those of them that are parts
+  int line, share;           // shares: the line's length for one key head, and a workgroup's share
+};
+
+constexpr float kComputeUnits = 256;
+constexpr int kNear = 4;     // a share ends at a row tile's end, or at least this many tiles from it
+
+template <int BM> __device__ __forceinline__ int line_at(const SeqWork& q, int r, int lead) {   // where row tile r of a sequence lies
+  const double slope = q.T > 1 ? 0.5 * (double)(q.v1 - q.v0) / (double)(q.T - 1) : 0.0;
+  return (int)floor((double)r * (double)(q.v0 + lead) + slope * (double)r * (double)(r - 1));
+}
+
+template <int BM, bool kShares> __device__ __forceinline__ PagedWork find_work(const PagedAttnArgs& a, const PagedSchedule& sc) {
+  const int lane = thread_id() & 63;
+  const auto add = [](float x, float y) { return x + y; };
+  const auto larger = [](float x, float y) { return fmaxf(x, y); };
+  float units = 0.0f, most = 0.0f, rows = 0.0f, longest = 1.0f;
+  SeqWork q;
+  for (int s0 = 0; s0 < a.n_seqs; s0 += kWave) {
+    q = seq_work<BM>(a, s0 + lane);
+    units += (float)q.T * 0.5f * (float)(q.v0 + q.v1);
+    most += (float)q.T * (float)max(q.v0, q.v1);
+    rows += (float)q.T;
+    longest = fmaxf(longest, (float)(q.T > 0 ? max(q.v0, q.v1) : 1));
+  }
+  PagedWork p = {false, 0x3fffffff, 0, 0, 0, 1};
+  if (sc.meets) {
+    units = total_of(units, 0.0f, add);
+    most = total_of(most, 0.0f, add);
+    rows = total_of(rows, 0.0f, add);
+    longest = total_of(longest, 0.0f, larger);
+    const float heads = (float)a.heads_kv, n = units / longest * heads;
     const float S = lane < 32 ? (float)(lane + 1) : floorf(32.0f * __builtin_amdgcn_exp2f((float)(lane - 31) * (5.0f / 32.0f)));   // .. 1024
-    const float x = n * S * (1.0f / kComputeUnits);
+    const float x = n * S * (1.0f / kComputeUnits), full = fminf(x, 1.0f);
     const float rounds = x <= 1.0f ? 1.0f : (units > 0.98f * longest * rows ? ceilf(x) : x + 0.75f);
-    float cost = rounds * (longest / S * fmaxf(sc.tile_alone, sc.tile * fminf(x, 1.0f)) + sc.start) + (lane > 0 ? sc.meet + sc.join * S : 0.0f);
-    if (lane > 0 && (most_units / longest * (float)a.heads_kv * S > (float)sc.target || S > longest)) cost = INFINITY;
-    float best = cost;
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) best = fminf(best, __shfl_xor(best, o, kWave));
+    float cost = rounds * (longest / S * fmaxf(sc.tile_alone + 0.3f * sc.tile * full, sc.tile * full) + sc.start) + (lane > 0 ? sc.meet + sc.join * S : 0.0f);
+    if (lane > 0 && (most / longest * heads * S > (float)sc.groups || S > longest)) cost = INFINITY;
+    const float best = -total_of(-cost, -INFINITY, larger);
     const int at = __ffsll(__ballot(cost == best)) - 1;
     const float s_best = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(S), at));
-    if (at > 0) C = __builtin_amdgcn_readfirstlane((int)ceilf(longest / s_best));
-  }
-  // items of one key head: the item's head, and its place among them
-  int each = 0, split_each = 0;
-  for (int s0 = 0; s0 < a.n_seqs; s0 += kWave) {
-    if (a.n_seqs > kWave) look(s0 + lane);
-    const int S = (w + C - 1) / C;
-    each += T * S;
-    split_each += S > 1 ? T * S : 0;
-  }
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    each += __shfl_xor(each, o, kWave);
-    split_each += __shfl_xor(split_each, o, kWave);
-  }
-  each = __builtin_amdgcn_readfirstlane(each);
-  split_each = __builtin_amdgcn_readfirstlane(split_each);
-  if (sc.by_xcd) {   // workgroup ids go round the XCDs: each takes one contiguous eighth of the items
-    const int per = (each * a.heads_kv + 7) / 8, slot = item >> 3;
-    if (slot >= per) return false;
-    item = (item & 7) * per + slot;
-  }
-  if (item >= each * a.heads_kv || split_each * a.heads_kv > sc.capacity) return false;   // (the latter cannot be, see above)
-  it.head_kv = item / each;
-  item -= it.head_kv * each;
-  int before = 0, split_before = 0;   // items and parts of the sequences before
-  for (int s0 = 0; s0 < a.n_seqs; s0 += kWave) {
-    if (a.n_seqs > kWave) look(s0 + lane);
-    const int S = (w + C - 1) / C, mine = T * S;
-    int upto = mine, split_upto = S > 1 ? mine : 0;
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-      const int u = __shfl_up(upto, o, kWave), v = __shfl_up(split_upto, o, kWave);
-      if (lane >= o) { upto += u; split_upto += v; }
+    if constexpr (kShares) {
+    const float line = (units + rows * (float)sc.lead) * heads;
+    const float by_shares = line * (1.0f / kComputeUnits) * sc.tile + 2.0f * sc.start + sc.meet + 3.0f * sc.join;
+    p.shares = line < 1e9f && line > (float)(sc.groups * (sc.lead + 3 * kNear)) && by_shares < best;
     }
-    const unsigned long long owner = __ballot(item >= before + upto - mine && item < before + upto);
+    if (!p.shares && at > 0) p.C = (int)ceilf(longest / s_best);
+  }
+  p.C = __builtin_amdgcn_readfirstlane(p.C);
+  p.shares = kShares && __builtin_amdgcn_readfirstlane((int)p.shares);
+  for (int s0 = 0; s0 < a.n_seqs; s0 += kWave) {
+    if (a.n_seqs > kWave) q = seq_work<BM>(a, s0 + lane);
+    if (p.shares) {
+      p.line += total_sum(line_at<BM>(q, q.T, sc.lead));
+    } else {
+      const int S = (max(q.v0, q.v1) + p.C - 1) / p.C;
+      p.each += total_sum(q.T * S);
+      p.split_each += total_sum(S > 1 ? q.T * S : 0);
+    }
+  }
+  if (p.shares) p.share = max((int)(((long long)p.line * a.heads_kv + sc.groups - 1) / sc.groups), sc.lead + 3 * kNear);
+  return p;
+}
+
+// What both ways have in common: the sequence that holds place y of `extent` a sequence, and what precedes it
+template <int BM, class Extent> __device__ __forceinline__ bool find_seq(const PagedAttnArgs& a, int y, Extent extent, SeqWork& q, int& seq, int& before,
+                                                                        int& split_before) {
+  const int lane = thread_id() & 63;
+  before = split_before = 0;
+  for (int s0 = 0; s0 < a.n_seqs; s0 += kWave) {
+    const SeqWork mine = seq_work<BM>(a, s0 + lane);
+    int split = 0;
+    const int e = extent(mine, split), upto = scan_sum(e), split_upto = scan_sum(split);
+    const unsigned long long owner = __ballot(y >= before + upto - e && y < before + upto);
     if (owner) {
       const int src = __ffsll(owner) - 1;
       auto of = [&](int v) { return __builtin_amdgcn_readlane(v, src); };
-      it.seq = s0 + src;
-      it.begin = of(begin);
-      it.m = of(m);
-      it.len = of(len);
-      it.held = min(it.len, most);
-      it.parts = of(S);
-      const int tiles = of(T), own = of(mine), idx = item - (before + of(upto) - own);
-      const int slot0 = it.head_kv * split_each + split_before + of(split_upto) - own;   // (meant where there are parts)
-      // within a sequence: part, then rows, the last ones (which see most) first
-      it.part = idx / tiles;
-      const int back = idx - it.part * tiles, r = tiles - 1 - back;
-      it.slot = slot0 + idx;
-      it.counter = slot0 + back;
-      it.first = r * BM;
-      it.rows = min(BM, it.m * group - it.first);
-      it.keys = key_tiles(a, it.m, it.len, it.held, it.first / group, (it.first + it.rows - 1) / group);
-      it.t0 = (int)((long long)it.keys.n * it.part / it.parts);
-      it.t1 = (int)((long long)it.keys.n * (it.part + 1) / it.parts);
+      q = SeqWork{of(mine.begin), of(mine.m), of(mine.len), of(mine.T), of(mine.v0), of(mine.v1)};
+      seq = s0 + src;
+      before += of(upto - e);
+      split_before += of(split_upto - split);
       return true;
     }
     before += __builtin_amdgcn_readlane(upto, 63);
     split_before += __builtin_amdgcn_readlane(split_upto, 63);
+  }
+  return false;
+}
+
+template <int BM> __device__ __forceinline__ void set_rows(const PagedAttnArgs& a, const SeqWork& q, int seq, int r, PagedItem& it) {
+  const int group = a.heads / a.heads_kv;
+  it.seq = seq;
+  it.begin = q.begin;
+  it.m = q.m;
+  it.len = q.len;
+  it.held = min(q.len, a.max_pages * a.page);
+  it.first = r * BM;
+  it.rows = min(BM, q.m * group - it.first);
+  it.keys = key_tiles(a, q.m, q.len, it.held, it.first / group, (it.first + it.rows - 1) / group);
+}
+
+// pieces: the `item`-th
+template <int BM> __device__ __forceinline__ bool find_piece(const PagedAttnArgs& a, const PagedSchedule& sc, const PagedWork& p, int item, PagedItem& it) {
+  if (item >= p.each * a.heads_kv || p.split_each * a.heads_kv > 2 * sc.groups) return false;   // (the latter cannot be)
+  it.head_kv = item / p.each;
+  const int y = item - it.head_kv * p.each;
+  auto parts = [&](const SeqWork& q) { return (max(q.v0, q.v1) + p.C - 1) / p.C; };
+  SeqWork q;
+  int seq, before, split_before;
+  if (!find_seq<BM>(a, y, [&](const SeqWork& x, int& split) {
+        const int S = parts(x);
+        split = S > 1 ? x.T * S : 0;
+        return x.T * S;
+      }, q, seq, before, split_before)) return false;
+  // within a sequence: part, then rows, the last ones (which see most) first
+  const int idx = y - before, back = idx % q.T;
+  it.part = idx / q.T;
+  it.parts = parts(q);
+  set_rows<BM>(a, q, seq, q.T - 1 - back, it);
+  it.counter = it.slot0 = it.head_kv * p.split_each + split_before + back;   // (meant where there are parts)
+  it.slot1 = it.slot0 + q.T;
+  it.slot_step = q.T;
+  it.t0 = (int)((long long)it.keys.n * it.part / it.parts);
+  it.t1 = (int)((long long)it.keys.n * (it.part + 1) / it.parts);
+  return true;
+}
+
+// shares: the part at place x of the line, if it is workgroup `wg`'s (parts of a row tile belong to consecutive ones); else, parts = 0.
+// next: where the row tile ends
+template <int BM> __device__ __forceinline__ bool find_part(const PagedAttnArgs& a, const PagedSchedule& sc, const PagedWork& p, int wg, int x, PagedItem& it,
+                                                           int& next) {
+  it.head_kv = x / p.line;
+  if (it.head_kv >= a.heads_kv) return false;
+  const int y = x - it.head_kv * p.line, lane = thread_id() & 63;
+  SeqWork q;
+  int seq, before, split_before;
+  if (!find_seq<BM>(a, y, [&](const SeqWork& s, int&) { return line_at<BM>(s, s.T, sc.lead); }, q, seq, before, split_before)) return false;
+  // the row tile: the last one that starts at or before y
+  int lo = 0, span = q.T;
+  while (span > 1) {
+    const int step = (span + kWave - 1) / kWave, r = lo + lane * step;
+    const int found = __popcll(__ballot(lane * step < span && line_at<BM>(q, r, sc.lead) <= y - before)) - 1;
+    lo += found * step;
+    span = min(step, span - found * step);
+  }
+  const int from = x - y + before + __builtin_amdgcn_readfirstlane(line_at<BM>(q, lo, sc.lead));
+  const int to = x - y + before + __builtin_amdgcn_readfirstlane(line_at<BM>(q, lo + 1, sc.lead));
+  next = to;
+  // the shares' ends g share that cut it: g = g0 .. g1
+  const int g0 = (from + sc.lead + kNear + p.share - 1) / p.share, g1 = (to - kNear) / p.share, cuts = max(0, g1 - g0 + 1);
+  it.part = min(max(x / p.share - g0 + 1, 0), cuts);
+  it.parts = cuts + 1;
+  if (g0 - 1 + it.part != wg) {
+    if (g0 - 1 + it.part > wg) return false;
+    it.parts = 0;
+    return true;
+  }
+  set_rows<BM>(a, q, seq, lo, it);
+  it.counter = g0 - 1;
+  it.slot0 = 2 * (g0 - 1) + 1;
+  it.slot1 = 2 * g0;
+  it.slot_step = 2;
+  auto tile_at = [&](int at) {   // of the row tile's n, at a place of the line
+    return (int)((double)max(0, at - from - sc.lead) * (double)it.keys.n / (double)max(1, to - from - sc.lead));
+  };
+  it.t0 = it.part == 0 ? 0 : tile_at((g0 + it.part - 1) * p.share);
+  it.t1 = it.part == cuts ? it.keys.n : tile_at((g0 + it.part) * p.share);
+  return true;
+}
+
+// the workgroup's items one after another: state, and a step to the next (false: there is none).  kStay: workgroups stay for more than one
+// and may have shares; else workgroup ids go round the XCDs so that each takes one contiguous eighth of the pieces, which read the same keys
+struct PagedCursor {
+  PagedWork work;
+  int at, end;
+};
+template <int BM, bool kStay> __device__ __forceinline__ PagedCursor first_item(const PagedAttnArgs& a, const PagedSchedule& sc) {
+  PagedCursor c;
+  c.work = find_work<BM, kStay>(a, sc);
+  const int id = (int)blockIdx.x;
+  if (!kStay) {   // (the grid is a multiple of eight, and has at least as many workgroups as there are pieces)
+    const int per = (c.work.each * a.heads_kv + 7) / 8;
+    c.at = (id & 7) * per + (id >> 3);
+    c.end = (id >> 3) < per ? c.at + 1 : c.at;
+  } else if (c.work.shares) {
+    c.at = id * c.work.share;
+    c.end = c.at + c.work.share;
+  } else {
+    c.at = id;
+    c.end = 0x7fffffff;
+  }
+  return c;
+}
+template <int BM, bool kStay> __device__ __forceinline__ bool next_item(const PagedAttnArgs& a, const PagedSchedule& sc, PagedCursor& c, PagedItem& it) {
+  if (!kStay || !c.work.shares) {
+    if (c.at >= c.end || !find_piece<BM>(a, sc, c.work, c.at, it)) return false;
+    c.at += (int)gridDim.x;
+    return true;
+  }
+  while (c.at < c.end) {
+    int next;
+    if (!find_part<BM>(a, sc, c.work, blockIdx.x, c.at, it, next)) return false;
+    const bool mine = it.parts > 0;
+    c.at = mine && it.part < it.parts - 1 ? c.end : next;   // (a cut is the share's end)
+    if (mine) return true;
   }
   return false;
 }
@@ -229,7 +388,7 @@ __device__ __forceinline__ bool any_bad_page(const PagedAttnArgs& a, const Paged
   bool bad = false;
   auto scan = [&](int t0, int t1) {   // tiles t0 .. t1 - 1
     const int last = div_page(a, min(it.keys.start(t1 - 1) + kKeyTile, it.held) - 1);
-    for (int e = div_page(a, it.keys.start(t0)) + (int)(threadIdx.x & 63); e <= last; e += kWave) bad = bad || !is_page(a, row[e]);
+    for (int e = div_page(a, it.keys.start(t0)) + (thread_id() & 63); e <= last; e += kWave) bad = bad || !is_page(a, row[e]);
   };
   if (it.t0 < it.keys.s1) scan(it.t0, min(it.t1, it.keys.s1));
   if (it.t1 > it.keys.s1) scan(max(it.t0, it.keys.s1), it.t1);
@@ -251,7 +410,7 @@ template <typename T, int D, int BM, int KS, int NT, class RowsAt, class StatsAt
 __device__ __forceinline__ void finish_item(const PagedAttnArgs& a, const PagedSchedule& sc, const PagedItem& it, RowsAt rows_at, StatsAt stats_at,
                                             int* flag) {
   constexpr int TPR = D / 8, PER = NT / TPR, PASS = (BM + PER - 1) / PER;
-  const int tid = threadIdx.x, f = 8 * (tid % TPR), r0 = tid / TPR, group = a.heads / a.heads_kv;
+  const int tid = thread_id(), f = 8 * (tid % TPR), r0 = tid / TPR, group = a.heads / a.heads_kv;
   typedef unsigned long long u64;
   __syncthreads();
   auto meet = [&](int row, float* acc, float& M, float& L) {   // the groups' parts of a row
@@ -315,8 +474,8 @@ __device__ __forceinline__ void finish_item(const PagedAttnArgs& a, const PagedS
   constexpr int kSc1 = 16;
   typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
   typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-  const __amdgpu_buffer_rsrc_t parts = __builtin_amdgcn_make_buffer_rsrc(sc.parts, 0, sc.capacity * (BM * (D + 2) * 4), 0x00020000);
-  const int stats_at_byte = sc.capacity * (BM * D * 4);
+  const __amdgpu_buffer_rsrc_t parts = __builtin_amdgcn_make_buffer_rsrc(sc.parts, 0, 2 * sc.groups * (BM * (D + 2) * 4), 0x00020000);
+  const int stats_at_byte = 2 * sc.groups * (BM * D * 4);
   auto row_byte = [&](int slot, int row) { return (slot * BM + row) * (D * 4) + 4 * f; };
   auto stat_byte = [&](int slot, int row) { return stats_at_byte + (slot * BM + row) * 8; };
   u64* const counter = sc.counters + it.counter;
@@ -331,10 +490,10 @@ __device__ __forceinline__ void finish_item(const PagedAttnArgs& a, const PagedS
     if (row >= it.rows) break;
     float acc[8], M, L;
     meet(row, acc, M, L);
-    const int to = row_byte(it.slot, row);
+    const int to = row_byte(it.slot(it.part), row);
     __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(acc[0]), __float_as_uint(acc[1]), __float_as_uint(acc[2]), __float_as_uint(acc[3])}, parts, to, 0, kSc1);
     __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(acc[4]), __float_as_uint(acc[5]), __float_as_uint(acc[6]), __float_as_uint(acc[7])}, parts, to + 16, 0, kSc1);
-    if (f == 0) __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(M), __float_as_uint(L)}, parts, stat_byte(it.slot, row), 0, kSc1);
+    if (f == 0) __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(M), __float_as_uint(L)}, parts, stat_byte(it.slot(it.part), row), 0, kSc1);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
@@ -346,9 +505,7 @@ __device__ __forceinline__ void finish_item(const PagedAttnArgs& a, const PagedS
   }
   __syncthreads();
   if (!*flag) return;
-  // ---- the last one.  The parts of (row tile, key head) lie as many slots apart as the sequence has row tiles.  Few rows leave threads
-  // over: G sets of threads then take every G-th part each and meet in LDS, in their order
-  const int tiles = (it.m * group + BM - 1) / BM;
+  // ---- the last one.  Few rows leave threads over: G sets of threads then take every G-th part each and meet in LDS, in their order
   int lanes_rows = 1;                                   // rows of a pass, a power of two
   while (lanes_rows < it.rows && lanes_rows < PER) lanes_rows *= 2;
   const int G = PER / lanes_rows, set = r0 / lanes_rows, rp = r0 % lanes_rows;
@@ -377,7 +534,7 @@ __device__ __forceinline__ void finish_item(const PagedAttnArgs& a, const PagedS
       for (int i = 0; i < U; ++i)
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-          const int slot = it.counter + min(u0 + i * G, it.parts - 1) * tiles;
+          const int slot = it.slot(min(u0 + i * G, it.parts - 1));
           st[r][i] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(parts, stat_byte(slot, row[r]), 0, kSc1));
           v[r][i][0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(parts, row_byte(slot, row[r]), 0, kSc1));
           v[r][i][1] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(parts, row_byte(slot, row[r]) + 16, 0, kSc1));

@@ -4,11 +4,13 @@
 //   S^T (keys x rows) = K_tile (A, from LDS) x Q^T (B, registers),   O^T (d x rows) += V_tile^T (A, LDS) x P^T (B, registers),
 // so that the statistics of a row are private to its two lanes and the exponentials of S^T are, rounded to bf16, the B operand of the
 // second product.  K and V tiles go global -> LDS directly, V^T fragments are transposing reads, three K slots and two V slots.
-// Here the rows are tokens x heads of a group, and a tile lies in pages: its descriptor is scalar arithmetic on an entry of the page table
-// that the scalar unit fetched a step before.
+// Here the rows are tokens x heads of a group, and a tile lies in pages.  A wavefront keeps 64 entries of the page table, a lane each; the
+// descriptor of a tile in one page is scalar arithmetic on one of them (read through the scalar unit instead, an entry is on its way when
+// the tile's barrier waits for everything that is: 12 heads x 4680 x 9360 0.33 ms).
 //
-// Two shapes of workgroup (NW wavefronts of rows, KS groups of wavefronts that share the keys):
-//   NW 4, KS 1   128 rows, tiles shared by four wavefronts, one barrier a tile: chunks, bound by the matrix cores and the softmax
+// Three shapes of workgroup (NW wavefronts of rows, KS groups of wavefronts that share the keys):
+//   NW 8, KS 1   256 rows, tiles shared by eight wavefronts, one barrier a tile, one workgroup a compute unit (head_dim 128): long chunks
+//   NW 4, KS 1   128 rows, two workgroups a compute unit (head_dim 64: three): chunks.  Both are bound by the matrix cores and the softmax
 //   NW 1, KS 4   32 rows, every wavefront its own tiles and no barrier until the end: single tokens, bound by memory
 #include "hf_paged_attn.h"
 
@@ -46,7 +48,7 @@ __device__ __forceinline__ float max3f(float a, float b, float c) {
 template <int D, int NW, int KS> struct Shape {
   static constexpr int BM = 32 * NW, NT = 64 * NW * KS;
   static constexpr int ROWB = 2 * D, TILE = kKeyTile * ROWB;
-  static constexpr int KSLOTS = NW == 4 ? 4 : 3;
+  static constexpr int KSLOTS = NW > 1 ? 4 : 3;
   static constexpr int GROUP = (KSLOTS + 2) * TILE;                  // a group's tiles: those of K, two of V
   static constexpr int OUT = BM * (D + 4) * 4 + BM * 8;              // a group's sums behind the loop, and its rows' statistics
   static constexpr int SPAN = GROUP > OUT ? GROUP : OUT;
@@ -54,10 +56,10 @@ template <int D, int NW, int KS> struct Shape {
   static constexpr int LDS = KS * SPAN + (GROUP > OUT ? 0 : 16);
 };
 
-// kBig: pages of 32 tokens and more: a tile lies in one page (one descriptor) or in two (an address per lane).  Else every piece of a tile
-// has a page of its own, or, where that ends inside a piece, every lane.
+// kBig: pages in which tiles lie whole, or nearly all do (of a multiple of 32 tokens, or of 256 and more): one descriptor a tile, or, over two
+// pages, an address per lane.  Else every lane has an address: pages may end anywhere.
 template <int D, int NW, int KS, bool kBig>
-__global__ __launch_bounds__(64 * NW * KS, (NW == 4 ? 2 : 1)) void paged_attn_kernel(const PagedLaunch) {
+__global__ __launch_bounds__(64 * NW * KS, (NW > 1 ? 2 : 1)) void paged_attn_kernel(const PagedLaunch) {
   static_assert(NW == 1 || KS == 1, "groups share no barrier");
   using S = Shape<D, NW, KS>;
   constexpr int BM = S::BM, ROWB = S::ROWB, TILE = S::TILE, KSLOTS = S::KSLOTS;
@@ -66,14 +68,21 @@ __global__ __launch_bounds__(64 * NW * KS, (NW == 4 ? 2 : 1)) void paged_attn_ke
   constexpr int NS = D / 16, ND = D / 32;                 // steps of S^T, 32-feature blocks of O^T
   extern __shared__ __attribute__((aligned(16))) char smem[];
 
+  PagedCursor cursor;
+  {
+    const PagedLaunch p = launch_arguments();
+    cursor = first_item<BM, NW == 1>(p.a, p.sc);
+  }
+  for (bool again = false;; again = true) {
   PagedItem it;
   {
     const PagedLaunch p = launch_arguments();
-    if (!find_item<BM>(p.a, p.sc, blockIdx.x, it)) return;
+    if (!next_item<BM, NW == 1>(p.a, p.sc, cursor, it)) return;
   }
+  if (again) __syncthreads();   // everybody is done with the sums in LDS
   const PagedAttnArgs a = launch_arguments().a;
 
-  const int tid = threadIdx.x, lane = tid & 63;
+  const int tid = thread_id(), lane = tid & 63;
   const int wave_in_wg = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wave = KS == 1 ? wave_in_wg : 0, grp = KS == 1 ? 0 : wave_in_wg;
   char* const sK = smem + grp * S::SPAN;
@@ -96,17 +105,26 @@ __global__ __launch_bounds__(64 * NW * KS, (NW == 4 ? 2 : 1)) void paged_attn_ke
   }
   const bool bad_pages = any_bad_page(a, it);
 
-  // ---- the item's tiles t0 + grp, + KS, ... (every wavefront of a group the same)
-  const int count = max(0, (it.t1 - it.t0 - grp + KS - 1) / KS);
+  // ---- the group's tiles (every wavefront of it the same): a run of the item's
+  const int per_group = (it.t1 - it.t0 + KS - 1) / KS, first_tile = it.t0 + grp * per_group;
+  const int count = max(0, min(per_group, it.t1 - first_tile));
   constexpr int kNone = 0x7fffffe0;                        // where no tile starts
-  auto start_of = [&](int i) { return i < count ? it.keys.start(it.t0 + grp + KS * i) : kNone; };
+  auto start_of = [&](int i) { return i < count ? it.keys.start(first_tile + i) : kNone; };
 
   // ---- requests: 1 KB pieces; piece j of this wavefront is the tile's keys RPP (wave + NW j) ..
   const uint32_t page_rows = (uint32_t)a.heads_kv * (uint32_t)a.page, head_rows = (uint32_t)it.head_kv * (uint32_t)a.page;   // (of the pool: < 2^32)
   const uint64_t k_pool = reinterpret_cast<uint64_t>(a.K_pages), v_pool = reinterpret_cast<uint64_t>(a.V_pages);
-  const ScalarInts table = (ScalarInts)(a.table + (long long)it.seq * a.max_pages);
+  const int32_t* const table = a.table + (long long)it.seq * a.max_pages;
   const uint32_t sK_lds = (uint32_t)(uintptr_t)sK, sV_lds = (uint32_t)(uintptr_t)sV;
-  const int key_last = it.held - 1;
+  const int key_last = it.held - 1, entry_last = it.held > 0 ? div_page(a, key_last) : 0;
+  // entries base .. base + 63 of the table, a lane each (-1 behind the sequence's last)
+  int ids = -1, ids_base = -kWave;
+  auto hold_pages = [&](int first, int last) {   // (uniform)
+    if (first < ids_base || last >= ids_base + kWave) {
+      ids_base = first;
+      ids = first + lane <= entry_last ? table[first + lane] : -1;
+    }
+  };
   auto row_at = [&](int id, int inside) { return (uint64_t)((uint32_t)id * page_rows + head_rows + (uint32_t)inside) * ROWB; };
   int k_off[CPT], v_off[CPT];
 #pragma unroll
@@ -127,58 +145,49 @@ __global__ __launch_bounds__(64 * NW * KS, (NW == 4 ? 2 : 1)) void paged_attn_ke
   };
   const uint64_t zeros = reinterpret_cast<uint64_t>(zero_row);
 
-  // The pages of a tile are asked for one step before its K is requested, its V is requested two steps after that.
-  // kBig: what was asked for (page, place in it) and what came of it (byte offset in the pool; bytes, -1: two pages)
-  struct Asked { int id[kBig ? 1 : CPT], inside; };
-  struct Place { uint64_t at; int bytes; };
-  auto ask = [&](Asked& p, int start) {
+  // Where a tile lies, found when its K is requested; its V is requested two steps after that.  kBig: byte offset in the pool and bytes
+  // (-1: two pages, which are looked up when they are needed).  Else: the lane's key (tile's key lane % 32), as a row of the pool, or kNoRow
+  struct Place { uint64_t at; int bytes; uint32_t row; };
+  constexpr uint32_t kNoRow = 0xffffffffu;
+  auto place_of = [&](int start) {
+    Place q = {0, 0, kNoRow};
+    if (start >= it.held) return q;   // (uniform)
+    const int entry = div_page(a, start), inside = start - entry * a.page;
     if constexpr (kBig) {
-      const int key = min(start, key_last), entry = div_page(a, key);
-      p.id[0] = table[entry];
-      p.inside = key - entry * a.page;
+      const int left = min(it.held - start, kKeyTile);
+      hold_pages(entry, entry);
+      const int id = __builtin_amdgcn_readlane(ids, entry - ids_base);
+      q.at = row_at(id, inside);
+      q.bytes = inside + left > a.page ? -1 : (is_page(a, id) ? left * ROWB : 0);
     } else {
-#pragma unroll
-      for (int j = 0; j < CPT; ++j) p.id[j] = table[div_page(a, min(start + RPP * (wave + NW * j), key_last))];
+      hold_pages(entry, div_page(a, min(start + kKeyTile - 1, key_last)));
+      const int key = min(start + l32, key_last), e = div_page(a, key), id = __shfl(ids, e - ids_base, kWave);
+      if (start + l32 < it.held && is_page(a, id)) q.row = (uint32_t)id * page_rows + head_rows + (uint32_t)(key - e * a.page);
     }
-  };
-  auto place_of = [&](const Asked& p, int start) {
-    const int left = min(max(it.held - start, 0), kKeyTile);
-    Place q;
-    q.at = is_page(a, p.id[0]) ? row_at(p.id[0], p.inside) : 0;
-    q.bytes = p.inside + left > a.page ? -1 : (is_page(a, p.id[0]) ? left * ROWB : 0);
     return q;
   };
   // the tile that starts at key `start` into the LDS at `slot`; keys that are none read as zeros
-  auto request_big = [&](uint64_t pool, const Place& q, uint32_t slot, int start, const int (&off)[CPT]) {
-    if (q.bytes >= 0) {   // (uniform)
+  auto request = [&](uint64_t pool, const Place& q, uint32_t slot, int start, const int (&off)[CPT]) {
+    if constexpr (kBig) {
+      if (q.bytes >= 0) {   // (uniform)
 #pragma unroll
-      for (int j = 0; j < CPT; ++j) to_lds(slot + (wave + NW * j) * 1024, off[j], pool + q.at, q.bytes);
+        for (int j = 0; j < CPT; ++j) to_lds(slot + (wave + NW * j) * 1024, off[j], pool + q.at, q.bytes);
+      } else {
+        const ScalarInts entries = (ScalarInts)table;
+        const int entry = div_page(a, start), cut = (entry + 1) * a.page - start, id0 = entries[entry], id1 = entries[entry + 1];
+        const uint64_t base0 = pool + row_at(id0, a.page - cut), base1 = pool + row_at(id1, 0) - (uint64_t)(uint32_t)(cut * ROWB);
+#pragma unroll
+        for (int j = 0; j < CPT; ++j) {
+          const int r = RPP * (wave + NW * j) + lane / UPR;
+          const bool ok = start + r < it.held && is_page(a, r < cut ? id0 : id1);
+          to_lds_from(slot + (wave + NW * j) * 1024, ok ? (r < cut ? base0 : base1) + (uint32_t)off[j] : zeros);
+        }
+      }
     } else {
-      const int entry = div_page(a, start), cut = (entry + 1) * a.page - start;
-      const int id0 = table[entry], id1 = table[entry + 1];   // (there are keys behind the cut)
-      const uint64_t base0 = is_page(a, id0) ? pool + row_at(id0, start - entry * a.page) : zeros;
-      const uint64_t base1 = is_page(a, id1) ? pool + row_at(id1, 0) - (uint64_t)(uint32_t)(cut * ROWB) : zeros;
 #pragma unroll
       for (int j = 0; j < CPT; ++j) {
-        const int r = RPP * (wave + NW * j) + lane / UPR;
-        const bool ok = start + r < it.held && is_page(a, r < cut ? id0 : id1);
-        to_lds_from(slot + (wave + NW * j) * 1024, ok ? (r < cut ? base0 : base1) + (uint32_t)off[j] : zeros);
-      }
-    }
-  };
-  auto request_small = [&](uint64_t pool, const Asked& p, uint32_t slot, int start, const int (&off)[CPT]) {
-    const int i = lane / UPR;
-#pragma unroll
-    for (int j = 0; j < CPT; ++j) {
-      const uint32_t dst = slot + (wave + NW * j) * 1024;
-      const int key = start + RPP * (wave + NW * j), left = min(RPP, it.held - key);
-      if (a.page % RPP == 0) {   // (uniform) the piece lies in one page
-        const int entry = div_page(a, min(key, key_last)), id = p.id[j];
-        const bool ok = left > 0 && is_page(a, id);
-        to_lds(dst, i * ROWB + off[j], ok ? pool + row_at(id, key - entry * a.page) : pool, ok ? left * ROWB : 0);
-      } else {
-        const int mine = min(key + i, max(key_last, 0)), entry = div_page(a, mine), id = a.table[(long long)it.seq * a.max_pages + entry];
-        to_lds_from(dst, i < left && is_page(a, id) ? pool + row_at(id, mine - entry * a.page) + (uint32_t)off[j] : zeros);
+        const uint32_t row = (uint32_t)__shfl((int)q.row, RPP * (wave + NW * j) + lane / UPR, kWave);
+        to_lds_from(slot + (wave + NW * j) * 1024, row != kNoRow ? pool + (uint64_t)row * ROWB + (uint32_t)off[j] : zeros);
       }
     }
   };
@@ -194,7 +203,7 @@ __global__ __launch_bounds__(64 * NW * KS, (NW == 4 ? 2 : 1)) void paged_attn_ke
     for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
       for (int y = 0; y < 2; ++y)   // (the swizzles of rows 16 apart agree)
-        v_addr[dt][y] = (key + 8 * y) * ROWB + 16 * ((4 * dt + 2 * g16 + ((j16 & 3) >> 1)) ^ v_swizzle<D>(key + 8 * y)) + 8 * (j16 & 1);
+        v_addr[dt][y] = sV_lds + (key + 8 * y) * ROWB + 16 * ((4 * dt + 2 * g16 + ((j16 & 3) >> 1)) ^ v_swizzle<D>(key + 8 * y)) + 8 * (j16 & 1);
   }
 
   f32x16 o[ND];
@@ -208,10 +217,9 @@ __global__ __launch_bounds__(64 * NW * KS, (NW == 4 ? 2 : 1)) void paged_attn_ke
 
   // Tiles by what the wavefront's rows see of them, in ranges of i (uniform): of those behind the sink's, every row sees all keys of
   // i_all .. i_all + n_all - 1; none sees any of those before i_some and behind i_end
-  const int i_window = max(0, (it.keys.s1 - it.t0 - grp + KS - 1) / KS);   // the first tile behind the sink's
-  auto first_from = [&](int key) {   // the first i >= i_window whose tile starts at `key` or behind
-    const int t = (key + kKeyTile - 1) / kKeyTile - it.keys.skip;
-    return max(i_window, (t - it.t0 - grp + KS - 1 + KS * 0x100000) / KS - 0x100000);
+  const int i_window = max(0, it.keys.s1 - first_tile);    // the first tile behind the sink's
+  auto first_from = [&](int key) {                         // the first i >= i_window whose tile starts at `key` or behind
+    return max(i_window, (key + kKeyTile - 1) / kKeyTile - it.keys.skip - first_tile);
   };
   const int i_some = first_from(view_lo.lo - (kKeyTile - 1)), i_end = active ? min(count, first_from(view_hi.hi)) : 0;
   const int i_all = first_from(view_hi.lo), n_all = bad_pages ? 0 : max(0, first_from(view_lo.hi - (kKeyTile - 1)) - i_all);
@@ -229,36 +237,17 @@ __global__ __launch_bounds__(64 * NW * KS, (NW == 4 ? 2 : 1)) void paged_attn_ke
 #pragma unroll
   for (int s = 0; s < NS; ++s) asm volatile("" : "+v"(qf[s]));
   int start1 = start_of(1), start2 = start_of(2), start3 = start_of(3);   // of tiles i + 1 .. i + 3
-  Asked asked_v, asked_k;                                                 // !kBig: tiles i + 1 and i + 3; kBig: asked_k is tile i + 4's
-  Place place1, place2, place3;                                           // kBig: of tiles i + 1 .. i + 3
+  Place place1 = {0, 0, kNoRow}, place2 = place1, place3 = place1;   // likewise
   if (count > 0) {
     const int start0 = start_of(0);
-    if constexpr (kBig) {
-      Asked p0, p1, p2, p3;
-      ask(p0, start0);
-      ask(p1, start1);
-      ask(p2, start2);
-      ask(p3, start3);
-      ask(asked_k, start_of(4));
-      const Place place0 = place_of(p0, start0);
-      place1 = place_of(p1, start1);
-      place2 = place_of(p2, start2);
-      place3 = place_of(p3, start3);
-      request_big(k_pool, place0, sK_lds, start0, k_off);
-      request_big(v_pool, place0, sV_lds, start0, v_off);
-      request_big(k_pool, place1, sK_lds + TILE, start1, k_off);
-      request_big(k_pool, place2, sK_lds + 2 * TILE, start2, k_off);
-    } else {
-      Asked p0, p2;
-      ask(p0, start0);
-      ask(asked_v, start1);
-      ask(p2, start2);
-      ask(asked_k, start3);
-      request_small(k_pool, p0, sK_lds, start0, k_off);
-      request_small(v_pool, p0, sV_lds, start0, v_off);
-      request_small(k_pool, asked_v, sK_lds + TILE, start1, k_off);
-      request_small(k_pool, p2, sK_lds + 2 * TILE, start2, k_off);
-    }
+    const Place place0 = place_of(start0);
+    place1 = place_of(start1);
+    place2 = place_of(start2);
+    place3 = place_of(start3);
+    request(k_pool, place0, sK_lds, start0, k_off);
+    request(v_pool, place0, sV_lds, start0, v_off);
+    request(k_pool, place1, sK_lds + TILE, start1, k_off);
+    request(k_pool, place2, sK_lds + 2 * TILE, start2, k_off);
   }
   asm volatile("s_waitcnt vmcnt(%0)" :: "n"(3 * CPT) : "memory");
   if (NW > 1) __syncthreads();
@@ -278,13 +267,11 @@ __global__ __launch_bounds__(64 * NW * KS, (NW == 4 ? 2 : 1)) void paged_attn_ke
     }
     asm volatile("s_waitcnt vmcnt(%0)" :: "n"(CPT) : "memory");   // K of tile i + 1 and V of tile i; K of i + 2 may fly
     if (NW > 1) __syncthreads();
-    if constexpr (kBig) request_big(v_pool, place1, sV_lds + (par ^ 1) * TILE, start1, v_off);
-    else request_small(v_pool, asked_v, sV_lds + (par ^ 1) * TILE, start1, v_off);
+    request(v_pool, place1, sV_lds + (par ^ 1) * TILE, start1, v_off);
     auto v_frag = [&](int dt, int t2) {
-      const char* p = sV + v_addr[dt][0] + par * TILE + 16 * ROWB * t2;
-      const char* q = sV + v_addr[dt][1] + par * TILE + 16 * ROWB * t2;
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(p));
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(q));
+      const uint32_t at = par * TILE + 16 * ROWB * t2;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(uintptr_t)(v_addr[dt][0] + at));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(uintptr_t)(v_addr[dt][1] + at));
       const s16x8 both = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
       return __builtin_bit_cast(bf16x8, both);
     };
@@ -362,8 +349,7 @@ __global__ __launch_bounds__(64 * NW * KS, (NW == 4 ? 2 : 1)) void paged_attn_ke
       for (int dt = 0; dt < ND; ++dt) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[dt], pf[0], o[dt], 0, 0, 0);
     }
     // (between the products: requests in a row queue up)
-    if constexpr (kBig) request_big(k_pool, place3, sK_lds + slot_new * TILE, start3, k_off);
-    else request_small(k_pool, asked_k, sK_lds + slot_new * TILE, start3, k_off);
+    request(k_pool, place3, sK_lds + slot_new * TILE, start3, k_off);
     if (some) {
 #pragma unroll
       for (int dt = 0; dt < ND; ++dt) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vg[dt], pf[1], o[dt], 0, 0, 0);
@@ -371,15 +357,9 @@ __global__ __launch_bounds__(64 * NW * KS, (NW == 4 ? 2 : 1)) void paged_attn_ke
     start1 = start2;
     start2 = start3;
     start3 = start_of(i + 4);
-    if constexpr (kBig) {
-      place1 = place2;
-      place2 = place3;
-      place3 = place_of(asked_k, start3);
-      ask(asked_k, start_of(i + 5));
-    } else {
-      ask(asked_v, start1);
-      ask(asked_k, start3);
-    }
+    place1 = place2;
+    place2 = place3;
+    place3 = place_of(start3);
   };
   if constexpr (KSLOTS == 4) {
     for (int i = 0; i < count; i += 4) {
@@ -457,60 +437,71 @@ __global__ __launch_bounds__(64 * NW * KS, (NW == 4 ? 2 : 1)) void paged_attn_ke
   finish_item<bf16_t, D, BM, KS, S::NT>(
       p.a, p.sc, it, [&](int u) { return reinterpret_cast<const float*>(smem + u * S::SPAN); },
       [&](int u) { return reinterpret_cast<const float*>(smem + u * S::SPAN) + BM * (D + 4); }, reinterpret_cast<int*>(smem + S::FLAG));
+  if constexpr (NW > 1) return;
+  }
 }
 
 // ---- launches
 struct Plan {
-  int rows, items, capacity;   // rows of a workgroup
+  int rows, grid;   // rows of a workgroup
   PagedSchedule sc;
 };
 
 Plan plan_of(const hf_paged& c, int n_q) {
   const int group = c.heads / c.heads_kv;
+  const long long rows = (long long)n_q * group;
   Plan p = {};
-  // a workgroup of 128 rows where a sequence has more than 32 on the average
-  p.rows = (long long)n_q * group > 32ll * c.n_seqs ? 128 : 32;
-  if (p.rows == 128) {
-    p.sc.target = 1536;
-    p.sc.tile = p.sc.tile_alone = 0.535f;
-    p.sc.start = 3.0f;
-    p.sc.meet = 6.0f;
-    p.sc.join = 0.5f;
-  } else {
-    p.sc.target = 1024;
+  auto tiles = [&](int of) { return (rows / of + (n_q < c.n_seqs ? n_q : c.n_seqs)) * c.heads_kv; };   // row tiles of all heads, at most
+  // A workgroup of 128 rows where a sequence has more than 32 on the average.  256 rows, whose tiles travel half as often, take 0.89 us a
+  // tile where two workgroups of 128 take 1.07, if a compute unit's rounds of them are no more.
+  p.rows = rows > 32ll * c.n_seqs ? 128 : 32;
+  if (p.rows == 128 && c.dtype == HF_BF16 && c.head_dim == 128 && rows > 128ll * c.n_seqs) {
+    const long long n = (rows + c.n_seqs - 1) / c.n_seqs, heads = (long long)c.n_seqs * c.heads_kv;   // (as if all were as long)
+    auto rounds = [&](int of) { return (double)(((n + of - 1) / of * heads + 255) / 256); };
+    if (rounds(256) * 0.89 <= rounds(128) * 0.535) p.rows = 256;
+  }
+  if (p.rows == 32) {
+    p.sc.groups = 256;
     p.sc.tile = 0.8f;
-    p.sc.tile_alone = 0.22f;
+    p.sc.tile_alone = 0.27f;
     p.sc.start = 4.0f;
     p.sc.meet = 5.0f;
     p.sc.join = 0.1f;
+    p.sc.lead = 5;
+  } else {
+    p.sc.groups = 131072 / p.rows / 2;
+    p.sc.tile = p.rows == 256 ? 0.89f : 0.535f;
+    p.sc.tile_alone = 0.7f * p.sc.tile;
+    p.sc.start = p.rows == 256 ? 9.0f : 5.0f;
+    p.sc.meet = 6.0f;
+    p.sc.join = 1.0f;
   }
-  p.sc.by_xcd = p.rows == 128;
-  const long long tiles = ((long long)n_q * group / p.rows + (n_q < c.n_seqs ? n_q : c.n_seqs)) * c.heads_kv;   // (at most)
-  const long long key_tiles = ((long long)c.max_pages * c.page_tokens + kKeyTile - 1) / kKeyTile;
-  const long long most = key_tiles < 1024 ? key_tiles : 1024;           // parts of a row tile
-  long long items = tiles + p.sc.target, parts = 2 * p.sc.target + 64;
-  if (items > tiles * most) items = tiles * most;
-  if (parts > tiles * most) parts = tiles * most;
-  p.items = (int)((items + 7) & ~7ll);
-  p.capacity = most > 1 ? (int)parts : 0;
+  const long long key_tiles = ((long long)c.max_pages * c.page_tokens + kKeyTile - 1) / kKeyTile;   // (at most)
+  long long grid = p.rows == 32 ? p.sc.groups : tiles(p.rows) + p.sc.groups;
+  if (grid > tiles(p.rows) * key_tiles) grid = tiles(p.rows) * key_tiles;
+  p.grid = (int)((grid + 7) & ~7ll);
+  p.sc.meets = key_tiles > 1;
   return p;
 }
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-template <int D, int NW, int KS, bool kBig> int launch(const PagedAttnArgs& a, const PagedSchedule& sc, int items, hipStream_t s) {
+template <int D, int NW, int KS, bool kBig> int launch(const PagedAttnArgs& a, const PagedSchedule& sc, int grid, hipStream_t s) {
   using S = Shape<D, NW, KS>;
   static LdsGrant grant;
   const int rc = grant_lds(grant, reinterpret_cast<const void*>(&paged_attn_kernel<D, NW, KS, kBig>), S::LDS, "hf_paged_attn_fwd");
   if (rc != HF_OK) return rc;
-  hipLaunchKernelGGL((paged_attn_kernel<D, NW, KS, kBig>), dim3(items), dim3(S::NT), S::LDS, s, PagedLaunch{a, sc});
+  hipLaunchKernelGGL((paged_attn_kernel<D, NW, KS, kBig>), dim3(grid), dim3(S::NT), S::LDS, s, PagedLaunch{a, sc});
   return check_launch("hf_paged_attn_fwd");
 }
 
 template <int D> int launch_of(const PagedAttnArgs& a, const PagedSchedule& sc, const Plan& p, hipStream_t s) {
-  const bool big = a.page >= kKeyTile;
-  if (p.rows == 128) return big ? launch<D, 4, 1, true>(a, sc, p.items, s) : launch<D, 4, 1, false>(a, sc, p.items, s);
-  return big ? launch<D, 1, 4, true>(a, sc, p.items, s) : launch<D, 1, 4, false>(a, sc, p.items, s);
+  const bool big = a.page % kKeyTile == 0 || a.page >= 256;
+  if constexpr (D == 128) {
+    if (p.rows == 256) return big ? launch<D, 8, 1, true>(a, sc, p.grid, s) : launch<D, 8, 1, false>(a, sc, p.grid, s);
+  }
+  if (p.rows == 128) return big ? launch<D, 4, 1, true>(a, sc, p.grid, s) : launch<D, 4, 1, false>(a, sc, p.grid, s);
+  return big ? launch<D, 1, 4, true>(a, sc, p.grid, s) : launch<D, 1, 4, false>(a, sc, p.grid, s);
 }
 
 }  // namespace
@@ -518,8 +509,8 @@ template <int D> int launch_of(const PagedAttnArgs& a, const PagedSchedule& sc, 
 size_t paged_workspace_bytes(const hf_paged& c, int n_q) {
   if (n_q == 0) return 0;
   const Plan p = plan_of(c, n_q);
-  if (p.capacity == 0) return 0;
-  return align256((size_t)p.capacity * 8) + align256((size_t)p.capacity * p.rows * (c.head_dim + 2) * 4);
+  if (!p.sc.meets) return 0;
+  return align256((size_t)p.sc.groups * 16) + (size_t)p.sc.groups * 2 * p.rows * (c.head_dim + 2) * 4;
 }
 
 int launch_paged_attn(const hf_paged& c, PagedAttnArgs a, void* workspace, hipStream_t s) {
@@ -529,13 +520,12 @@ int launch_paged_attn(const hf_paged& c, PagedAttnArgs a, void* workspace, hipSt
   a.page_shift = 31 + shift;
   a.page_magic = (uint32_t)((1ull << a.page_shift) / (unsigned)c.page_tokens + 1);
   PagedSchedule sc = p.sc;
-  sc.capacity = p.capacity;
-  if (p.capacity > 0) {
+  if (sc.meets) {
     sc.counters = static_cast<unsigned long long*>(workspace);
-    sc.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + align256((size_t)p.capacity * 8));
+    sc.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + align256((size_t)sc.groups * 16));
     sc.tag = next_call_tag();
   }
-  if (c.dtype == HF_F32) return launch_paged_attn_f32(c, a, sc, p.rows, p.items, s);
+  if (c.dtype == HF_F32) return launch_paged_attn_f32(c, a, sc, p.rows, p.grid, s);
   return c.head_dim == 128 ? launch_of<128>(a, sc, p, s) : launch_of<64>(a, sc, p, s);
 }
 

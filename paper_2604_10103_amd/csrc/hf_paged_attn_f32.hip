@@ -25,13 +25,21 @@ __global__ __launch_bounds__(64 * NW * KS, 1) void paged_attn_f32_kernel(const P
   extern __shared__ __attribute__((aligned(16))) float sums[];
   typedef float piece __attribute__((ext_vector_type(E)));
 
+  PagedCursor cursor;
+  {
+    const PagedLaunch p = launch_arguments();
+    cursor = first_item<BM, NW == 1>(p.a, p.sc);
+  }
+  for (bool again = false;; again = true) {
   PagedItem it;
   {
     const PagedLaunch p = launch_arguments();
-    if (!find_item<BM>(p.a, p.sc, blockIdx.x, it)) return;
+    if (!next_item<BM, NW == 1>(p.a, p.sc, cursor, it)) return;
   }
+  if (again) __syncthreads();   // everybody is done with the sums in LDS
   const PagedAttnArgs a = launch_arguments().a;
-  const int tid = threadIdx.x, lane = tid & 63;
+
+  const int tid = thread_id(), lane = tid & 63;
   const int wave_in_wg = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wave = wave_in_wg % NW, grp = wave_in_wg / NW;
   const int l32 = lane & 31, h = lane >> 5, group = a.heads / a.heads_kv;
@@ -210,22 +218,24 @@ __global__ __launch_bounds__(64 * NW * KS, 1) void paged_attn_f32_kernel(const P
   const PagedLaunch p = launch_arguments();
   finish_item<float, D, BM, KS, NT>(p.a, p.sc, it, [&](int u) { return sums + u * SPAN; }, [&](int u) { return sums + u * SPAN + BM * (D + 4); },
                                     reinterpret_cast<int*>(sums + KS * SPAN));
+  if constexpr (NW > 1) return;
+  }
 }
 
-template <int D, int NW, int KS> int launch(const PagedAttnArgs& a, const PagedSchedule& sc, int items, hipStream_t s) {
+template <int D, int NW, int KS> int launch(const PagedAttnArgs& a, const PagedSchedule& sc, int grid, hipStream_t s) {
   constexpr int kLds = KS * (32 * NW * (D + 4) + 64 * NW) * 4 + 16;
   static LdsGrant grant;
   const int rc = grant_lds(grant, reinterpret_cast<const void*>(&paged_attn_f32_kernel<D, NW, KS>), kLds, "hf_paged_attn_fwd");
   if (rc != HF_OK) return rc;
-  hipLaunchKernelGGL((paged_attn_f32_kernel<D, NW, KS>), dim3(items), dim3(64 * NW * KS), kLds, s, PagedLaunch{a, sc});
+  hipLaunchKernelGGL((paged_attn_f32_kernel<D, NW, KS>), dim3(grid), dim3(64 * NW * KS), kLds, s, PagedLaunch{a, sc});
   return check_launch("hf_paged_attn_fwd");
 }
 
 }  // namespace
 
-int launch_paged_attn_f32(const hf_paged& c, const PagedAttnArgs& a, const PagedSchedule& sc, int rows, int items, hipStream_t s) {
-  if (c.head_dim == 128) return rows == 128 ? launch<128, 4, 1>(a, sc, items, s) : launch<128, 1, 4>(a, sc, items, s);
-  return rows == 128 ? launch<64, 4, 1>(a, sc, items, s) : launch<64, 1, 4>(a, sc, items, s);
+int launch_paged_attn_f32(const hf_paged& c, const PagedAttnArgs& a, const PagedSchedule& sc, int rows, int grid, hipStream_t s) {
+  if (c.head_dim == 128) return rows == 128 ? launch<128, 4, 1>(a, sc, grid, s) : launch<128, 1, 4>(a, sc, grid, s);
+  return rows == 128 ? launch<64, 4, 1>(a, sc, grid, s) : launch<64, 1, 4>(a, sc, grid, s);
 }
 
 }  // namespace hf
