@@ -86,7 +86,6 @@ __global__ __launch_bounds__(64 * NW * KS, (NW > 1 ? 2 : 1)) void paged_attn_ker
   const int wave_in_wg = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wave = KS == 1 ? wave_in_wg : 0, grp = KS == 1 ? 0 : wave_in_wg;
   char* const sK = smem + grp * S::SPAN;
-  char* const sV = sK + KSLOTS * TILE;
   const int l32 = lane & 31, h = lane >> 5, group = a.heads / a.heads_kv;
 
   // ---- this lane's row (past the item's rows: its last one again; only the rows that there are get stored)
@@ -105,32 +104,25 @@ __global__ __launch_bounds__(64 * NW * KS, (NW > 1 ? 2 : 1)) void paged_attn_ker
   }
   const bool bad_pages = any_bad_page(a, it);
 
-  // ---- the group's tiles (every wavefront of it the same): a run of the item's
-  const int per_group = (it.t1 - it.t0 + KS - 1) / KS, first_tile = it.t0 + grp * per_group;
-  const int count = max(0, min(per_group, it.t1 - first_tile));
-  constexpr int kNone = 0x7fffffe0;                        // where no tile starts
-  auto start_of = [&](int i) { return i < count ? it.keys.start(first_tile + i) : kNone; };
+  // ---- the group's tiles, every wavefront of it the same: every KS-th of the item's, or (pages by lane) a run of them, whose pages are fewer
+  constexpr int kStride = kBig ? KS : 1;
+  const int run = (it.t1 - it.t0 + KS - 1) / KS, base_tile = it.t0 + grp * (kBig ? 1 : run);
+  const int count = kBig ? max(0, (it.t1 - base_tile + KS - 1) / KS) : max(0, min(run, it.t1 - base_tile));
+  auto start_of = [&](int i) { return it.keys.start(base_tile + kStride * i); };   // (0 <= i < count)
 
-  // ---- requests: 1 KB pieces; piece j of this wavefront is the tile's keys RPP (wave + NW j) ..
+  // ---- requests: 1 KB pieces; piece j of this wavefront is the tile's keys RPP (wave + NW j) ..  Keys that are none read as zeros
   const uint32_t page_rows = (uint32_t)a.heads_kv * (uint32_t)a.page, head_rows = (uint32_t)it.head_kv * (uint32_t)a.page;   // (of the pool: < 2^32)
   const uint64_t k_pool = reinterpret_cast<uint64_t>(a.K_pages), v_pool = reinterpret_cast<uint64_t>(a.V_pages);
   const int32_t* const table = a.table + (long long)it.seq * a.max_pages;
-  const uint32_t sK_lds = (uint32_t)(uintptr_t)sK, sV_lds = (uint32_t)(uintptr_t)sV;
-  const int key_last = it.held - 1, entry_last = it.held > 0 ? div_page(a, key_last) : 0;
-  // entries base .. base + 63 of the table, a lane each (-1 behind the sequence's last)
-  int ids = -1, ids_base = -kWave;
-  auto hold_pages = [&](int first, int last) {   // (uniform)
-    if (first < ids_base || last >= ids_base + kWave) {
-      ids_base = first;
-      ids = first + lane <= entry_last ? table[first + lane] : -1;
-    }
-  };
-  auto row_at = [&](int id, int inside) { return (uint64_t)((uint32_t)id * page_rows + head_rows + (uint32_t)inside) * ROWB; };
+  typedef __attribute__((address_space(3))) char* Lds;
+  const uint32_t sK_lds = (uint32_t)(uintptr_t)(Lds)smem + grp * S::SPAN, sV_lds = sK_lds + KSLOTS * TILE;
+  const int key_last = it.held - 1;
+  const uint64_t zeros = reinterpret_cast<uint64_t>(zero_row);
   int k_off[CPT], v_off[CPT];
 #pragma unroll
   for (int j = 0; j < CPT; ++j) {
     const int r = RPP * (wave + NW * j) + lane / UPR, u = lane % UPR;
-    const int row = kBig ? r * ROWB : 0;   // (from the tile's first key, or none: a lane's place in its piece is added where it is needed)
+    const int row = kBig ? r * ROWB : 0;   // (from the tile's first key; by lane: the key's own row is added)
     k_off[j] = row + ((u ^ k_swizzle<D>(r)) * 16);
     v_off[j] = row + ((u ^ v_swizzle<D>(r)) * 16);
   }
@@ -143,52 +135,84 @@ __global__ __launch_bounds__(64 * NW * KS, (NW > 1 ? 2 : 1)) void paged_attn_ker
                         __builtin_amdgcn_readfirstlane(bytes), 0x00020000};
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(dst), "v"(off), "s"(desc) : "memory", "m0");
   };
-  const uint64_t zeros = reinterpret_cast<uint64_t>(zero_row);
+  auto pool_row = [&](int id, int inside) { return (uint32_t)id * page_rows + head_rows + (uint32_t)inside; };
 
-  // Where a tile lies, found when its K is requested; its V is requested two steps after that.  kBig: byte offset in the pool and bytes
-  // (-1: two pages, which are looked up when they are needed).  Else: the lane's key (tile's key lane % 32), as a row of the pool, or kNoRow
-  struct Place { uint64_t at; int bytes; uint32_t row; };
-  constexpr uint32_t kNoRow = 0xffffffffu;
-  auto place_of = [&](int start) {
-    Place q = {0, 0, kNoRow};
-    if (start >= it.held) return q;   // (uniform)
-    const int entry = div_page(a, start), inside = start - entry * a.page;
-    if constexpr (kBig) {
-      const int left = min(it.held - start, kKeyTile);
-      hold_pages(entry, entry);
-      const int id = __builtin_amdgcn_readlane(ids, entry - ids_base);
-      q.at = row_at(id, inside);
-      q.bytes = inside + left > a.page ? -1 : (is_page(a, id) ? left * ROWB : 0);
-    } else {
-      hold_pages(entry, div_page(a, min(start + kKeyTile - 1, key_last)));
-      const int key = min(start + l32, key_last), e = div_page(a, key), id = __shfl(ids, e - ids_base, kWave);
-      if (start + l32 < it.held && is_page(a, id)) q.row = (uint32_t)id * page_rows + head_rows + (uint32_t)(key - e * a.page);
+  // kBig: where 64 tiles lie, a lane each: the pool's row of the first key, and how many bytes (-1: they go on in another page).  Of the
+  // tiles that K is requested for, and of those that V is, which come two later
+  struct Places { uint32_t row; int bytes; };
+  Places k_places = {0, 0}, v_places = {0, 0};
+  auto find_places = [&](int i0) {
+    const int i = i0 + lane, start = i < count ? start_of(i) : it.held;
+    k_places = {0, 0};
+    if (start < it.held) {
+      const int entry = div_page(a, start), inside = start - entry * a.page, left = min(it.held - start, kKeyTile), id = table[entry];
+      k_places.row = pool_row(id, inside);
+      k_places.bytes = inside + left > a.page ? -1 : (is_page(a, id) ? left * ROWB : 0);
     }
-    return q;
   };
-  // the tile that starts at key `start` into the LDS at `slot`; keys that are none read as zeros
-  auto request = [&](uint64_t pool, const Place& q, uint32_t slot, int start, const int (&off)[CPT]) {
-    if constexpr (kBig) {
-      if (q.bytes >= 0) {   // (uniform)
+  auto request_big = [&](uint64_t pool, const Places& p, int i, uint32_t slot, const int (&off)[CPT]) {
+    const int bytes = __builtin_amdgcn_readlane(p.bytes, i & 63);
+    const uint32_t row = __builtin_amdgcn_readlane(p.row, i & 63);
+    const uint64_t base = pool + (uint64_t)row * ROWB;
+    if (bytes >= 0) {   // (uniform)
 #pragma unroll
-        for (int j = 0; j < CPT; ++j) to_lds(slot + (wave + NW * j) * 1024, off[j], pool + q.at, q.bytes);
-      } else {
-        const ScalarInts entries = (ScalarInts)table;
-        const int entry = div_page(a, start), cut = (entry + 1) * a.page - start, id0 = entries[entry], id1 = entries[entry + 1];
-        const uint64_t base0 = pool + row_at(id0, a.page - cut), base1 = pool + row_at(id1, 0) - (uint64_t)(uint32_t)(cut * ROWB);
-#pragma unroll
-        for (int j = 0; j < CPT; ++j) {
-          const int r = RPP * (wave + NW * j) + lane / UPR;
-          const bool ok = start + r < it.held && is_page(a, r < cut ? id0 : id1);
-          to_lds_from(slot + (wave + NW * j) * 1024, ok ? (r < cut ? base0 : base1) + (uint32_t)off[j] : zeros);
-        }
-      }
-    } else {
+      for (int j = 0; j < CPT; ++j) to_lds(slot + (wave + NW * j) * 1024, off[j], base, bytes);
+    } else {            // two pages: an address per lane
+      const ScalarInts entries = (ScalarInts)table;
+      int start = start_of(i);
+      asm volatile("" : "+s"(start));   // (what follows stays behind the branch)
+      const int entry = div_page(a, start), cut = (entry + 1) * a.page - start, id0 = entries[entry], id1 = entries[entry + 1];
+      const uint64_t next = pool + (uint64_t)pool_row(id1, 0) * ROWB - (uint64_t)(uint32_t)(cut * ROWB);
 #pragma unroll
       for (int j = 0; j < CPT; ++j) {
-        const uint32_t row = (uint32_t)__shfl((int)q.row, RPP * (wave + NW * j) + lane / UPR, kWave);
-        to_lds_from(slot + (wave + NW * j) * 1024, row != kNoRow ? pool + (uint64_t)row * ROWB + (uint32_t)off[j] : zeros);
+        const int r = RPP * (wave + NW * j) + lane / UPR;
+        const bool ok = start + r < it.held && is_page(a, r < cut ? id0 : id1);
+        to_lds_from(slot + (wave + NW * j) * 1024, ok ? (r < cut ? base : next) + (uint32_t)off[j] : zeros);
       }
+    }
+  };
+  // else: the pool's row of the lane's key (the tile's key lane % 32), kNoRow: none; of tiles i + 1 .. i + 3.  The wavefront keeps 64 entries
+  // of the table, from ids_base on, a lane each
+  constexpr uint32_t kNoRow = 0xffffffffu;
+  uint32_t row1 = kNoRow, row2 = kNoRow, row3 = kNoRow;
+  int ids = -1, ids_base = -kWave;
+  const int entry_last = it.held > 0 ? div_page(a, key_last) : 0;
+  auto rows_of = [&](int i) {
+    const int start = i < count ? start_of(i) : it.held;
+    if (start >= it.held) return kNoRow;   // (uniform)
+    const int first = div_page(a, start), last = div_page(a, min(start + kKeyTile - 1, key_last));
+    if (first < ids_base || last >= ids_base + kWave) {
+      ids_base = first;
+      ids = first + lane <= entry_last ? table[first + lane] : -1;
+    }
+    const int key = min(start + l32, key_last), entry = div_page(a, key), id = __shfl(ids, entry - ids_base, kWave);
+    return start + l32 < it.held && is_page(a, id) ? pool_row(id, key - entry * a.page) : kNoRow;
+  };
+  auto request_rows = [&](uint64_t pool, uint32_t rows, uint32_t slot, const int (&off)[CPT]) {
+#pragma unroll
+    for (int j = 0; j < CPT; ++j) {
+      const uint32_t row = (uint32_t)__shfl((int)rows, RPP * (wave + NW * j) + lane / UPR, kWave);
+      to_lds_from(slot + (wave + NW * j) * 1024, row != kNoRow ? pool + (uint64_t)row * ROWB + (uint32_t)off[j] : zeros);
+    }
+  };
+  // V of tile i + 1 and K of tile i + 3, whose turn it is in step i
+  auto request_v = [&](int i, uint32_t slot) {
+    if constexpr (kBig) {
+      if (((i + 1) & 63) == 0) v_places = k_places;
+      request_big(v_pool, v_places, i + 1, slot, v_off);
+    } else {
+      request_rows(v_pool, row1, slot, v_off);
+    }
+  };
+  auto request_k = [&](int i, uint32_t slot) {
+    if constexpr (kBig) {
+      if (((i + 3) & 63) == 0) find_places(i + 3);
+      request_big(k_pool, k_places, i + 3, slot, k_off);
+    } else {
+      request_rows(k_pool, row3, slot, k_off);
+      row1 = row2;
+      row2 = row3;
+      row3 = rows_of(i + 4);
     }
   };
 
@@ -215,15 +239,12 @@ __global__ __launch_bounds__(64 * NW * KS, (NW > 1 ? 2 : 1)) void paged_attn_ker
   uint32_t seen = 0;
   bool odd = false;   // values that are not finite lie next to rows that do not see them: they were left out (uniform)
 
-  // Tiles by what the wavefront's rows see of them, in ranges of i (uniform): of those behind the sink's, every row sees all keys of
-  // i_all .. i_all + n_all - 1; none sees any of those before i_some and behind i_end
-  const int i_window = max(0, it.keys.s1 - first_tile);    // the first tile behind the sink's
-  auto first_from = [&](int key) {                         // the first i >= i_window whose tile starts at `key` or behind
-    return max(i_window, (key + kKeyTile - 1) / kKeyTile - it.keys.skip - first_tile);
+  // the tiles of which every row of the wavefront sees all keys (uniform): i_all .. i_all + n_all - 1, behind the sink's
+  auto first_from = [&](int key) {   // the first i whose tile lies behind the sink's and starts at `key` or behind
+    const int t = max(it.keys.s1, (key + kKeyTile - 1) / kKeyTile - it.keys.skip) - base_tile;
+    return t <= 0 ? 0 : (t + kStride - 1) / kStride;
   };
-  const int i_some = first_from(view_lo.lo - (kKeyTile - 1)), i_end = active ? min(count, first_from(view_hi.hi)) : 0;
   const int i_all = first_from(view_hi.lo), n_all = bad_pages ? 0 : max(0, first_from(view_lo.hi - (kKeyTile - 1)) - i_all);
-  auto some_of = [&](int i) { return i < i_end && (i >= i_some || i < i_window); };
   auto all_of = [&](int i) { return (unsigned)(i - i_all) < (unsigned)n_all; };
   // the tile's keys that lie in pages, a bit each
   auto existing = [&](int start) {
@@ -236,18 +257,24 @@ __global__ __launch_bounds__(64 * NW * KS, (NW > 1 ? 2 : 1)) void paged_attn_ker
   // all of them
 #pragma unroll
   for (int s = 0; s < NS; ++s) asm volatile("" : "+v"(qf[s]));
-  int start1 = start_of(1), start2 = start_of(2), start3 = start_of(3);   // of tiles i + 1 .. i + 3
-  Place place1 = {0, 0, kNoRow}, place2 = place1, place3 = place1;   // likewise
   if (count > 0) {
-    const int start0 = start_of(0);
-    const Place place0 = place_of(start0);
-    place1 = place_of(start1);
-    place2 = place_of(start2);
-    place3 = place_of(start3);
-    request(k_pool, place0, sK_lds, start0, k_off);
-    request(v_pool, place0, sV_lds, start0, v_off);
-    request(k_pool, place1, sK_lds + TILE, start1, k_off);
-    request(k_pool, place2, sK_lds + 2 * TILE, start2, k_off);
+    if constexpr (kBig) {
+      find_places(0);
+      v_places = k_places;
+      request_big(k_pool, k_places, 0, sK_lds, k_off);
+      request_big(v_pool, k_places, 0, sV_lds, v_off);
+      request_big(k_pool, k_places, 1, sK_lds + TILE, k_off);
+      request_big(k_pool, k_places, 2, sK_lds + 2 * TILE, k_off);
+    } else {
+      const uint32_t row0 = rows_of(0);
+      row1 = rows_of(1);
+      row2 = rows_of(2);
+      row3 = rows_of(3);
+      request_rows(k_pool, row0, sK_lds, k_off);
+      request_rows(v_pool, row0, sV_lds, v_off);
+      request_rows(k_pool, row1, sK_lds + TILE, k_off);
+      request_rows(k_pool, row2, sK_lds + 2 * TILE, k_off);
+    }
   }
   asm volatile("s_waitcnt vmcnt(%0)" :: "n"(3 * CPT) : "memory");
   if (NW > 1) __syncthreads();
@@ -257,17 +284,14 @@ __global__ __launch_bounds__(64 * NW * KS, (NW > 1 ? 2 : 1)) void paged_attn_ker
 
   // tile i: its K fragments are in registers; slot_next, slot_new: where K of tiles i + 1 and i + 3 lie; par: V slot of tile i
   auto step = [&](int i, const int slot_next, const int slot_new, const int par) {
-    const bool some = some_of(i);
     f32x16 sacc;
-    if (some) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) sacc[r] = 0.0f;
+    for (int r = 0; r < 16; ++r) sacc[r] = 0.0f;
 #pragma unroll
-      for (int s = 0; s < NS; ++s) sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s], qf[s], sacc, 0, 0, 0);
-    }
+    for (int s = 0; s < NS; ++s) sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s], qf[s], sacc, 0, 0, 0);
     asm volatile("s_waitcnt vmcnt(%0)" :: "n"(CPT) : "memory");   // K of tile i + 1 and V of tile i; K of i + 2 may fly
     if (NW > 1) __syncthreads();
-    request(v_pool, place1, sV_lds + (par ^ 1) * TILE, start1, v_off);
+    request_v(i, sV_lds + (par ^ 1) * TILE);
     auto v_frag = [&](int dt, int t2) {
       const uint32_t at = par * TILE + 16 * ROWB * t2;
       const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(uintptr_t)(v_addr[dt][0] + at));
@@ -276,16 +300,14 @@ __global__ __launch_bounds__(64 * NW * KS, (NW > 1 ? 2 : 1)) void paged_attn_ker
       return __builtin_bit_cast(bf16x8, both);
     };
     bf16x8 vf[ND], vg[ND], pf[2];
-    if (some) {
 #pragma unroll
-      for (int dt = 0; dt < ND; ++dt) vf[dt] = v_frag(dt, 0);
+    for (int dt = 0; dt < ND; ++dt) vf[dt] = v_frag(dt, 0);
 #pragma unroll
-      for (int dt = 0; dt < ND; ++dt) vg[dt] = v_frag(dt, 1);
-    }
+    for (int dt = 0; dt < ND; ++dt) vg[dt] = v_frag(dt, 1);
 #pragma unroll
     for (int s = 0; s < NS; ++s) kf[s] = *reinterpret_cast<const bf16x8*>(sK + k_addr[s] + slot_next * TILE);
     __builtin_amdgcn_sched_barrier(0);
-    if (some) {
+    {
       if (!all_of(i)) {
         const int start = start_of(i);
         const uint32_t sees = view.sees_tile(start) & existing(start), mine = sees >> (4 * h);
@@ -348,20 +370,18 @@ __global__ __launch_bounds__(64 * NW * KS, (NW > 1 ? 2 : 1)) void paged_attn_ker
 #pragma unroll
       for (int dt = 0; dt < ND; ++dt) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[dt], pf[0], o[dt], 0, 0, 0);
     }
-    // (between the products: requests in a row queue up)
-    request(k_pool, place3, sK_lds + slot_new * TILE, start3, k_off);
-    if (some) {
+    request_k(i, sK_lds + slot_new * TILE);   // (between the products: requests in a row queue up)
 #pragma unroll
-      for (int dt = 0; dt < ND; ++dt) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vg[dt], pf[1], o[dt], 0, 0, 0);
-    }
-    start1 = start2;
-    start2 = start3;
-    start3 = start_of(i + 4);
-    place1 = place2;
-    place2 = place3;
-    place3 = place_of(start3);
+    for (int dt = 0; dt < ND; ++dt) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vg[dt], pf[1], o[dt], 0, 0, 0);
   };
-  if constexpr (KSLOTS == 4) {
+  if constexpr (NW == 1) {
+    int slot = 0;
+    for (int i = 0; i < count; ++i) {   // (the step that frees slot i mod 3 fills it with tile i + 3)
+      const int next = slot == 2 ? 0 : slot + 1;
+      step(i, next, slot, i & 1);
+      slot = next;
+    }
+  } else if (active) {
     for (int i = 0; i < count; i += 4) {
       step(i, 1, 3, 0);
       if (i + 1 >= count) break;
@@ -371,12 +391,12 @@ __global__ __launch_bounds__(64 * NW * KS, (NW > 1 ? 2 : 1)) void paged_attn_ker
       if (i + 3 >= count) break;
       step(i + 3, 0, 2, 1);
     }
-  } else {
-    int slot = 0;
-    for (int i = 0; i < count; ++i) {   // (the step that frees slot i mod 3 fills it with tile i + 3)
-      const int next = slot == 2 ? 0 : slot + 1;
-      step(i, next, slot, i & 1);
-      slot = next;
+  } else {   // no rows: the wavefront only carries its share of the tiles
+    for (int i = 0; i < count; ++i) {
+      asm volatile("s_waitcnt vmcnt(%0)" :: "n"(CPT) : "memory");
+      __syncthreads();
+      request_v(i, sV_lds + ((i & 1) ^ 1) * TILE);
+      request_k(i, sK_lds + ((i + 3) & 3) * TILE);
     }
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing may land on the sums
@@ -388,7 +408,7 @@ __global__ __launch_bounds__(64 * NW * KS, (NW > 1 ? 2 : 1)) void paged_attn_ker
     const float m_use = m_ref == -INFINITY ? 0.0f : m_ref;
 #pragma unroll 1
     for (int i = 0; i < count; ++i) {
-      if (!some_of(i) || all_of(i)) continue;
+      if (all_of(i)) continue;
       const int start = start_of(i);
 #pragma unroll 1
       for (int k = 0; k < kKeyTile; ++k) {
@@ -396,7 +416,7 @@ __global__ __launch_bounds__(64 * NW * KS, (NW > 1 ? 2 : 1)) void paged_attn_ker
         if (key >= it.held) break;
         const int entry = div_page(a, key), id = table[entry];
         if (!is_page(a, id)) continue;
-        const uint64_t at = row_at(id, key - entry * a.page);
+        const uint64_t at = (uint64_t)pool_row(id, key - entry * a.page) * ROWB;
         float s = 0.0f;
 #pragma unroll
         for (int c = 0; c < NS; ++c) {
