@@ -21,6 +21,9 @@ struct PagedAttnArgs {
   float c_scale;              // softmax_scale * log2(e)
   uint32_t page_magic;        // key / page = key * page_magic >> page_shift for key < 2^31
   int page_shift;
+  int page_tiles;             // > 0: key tiles end with their page, of which there are so many in one; tile / page_tiles as above
+  uint32_t tiles_magic;
+  int tiles_shift;
 };
 size_t paged_workspace_bytes(const hf_paged& c, int n_q);
 int launch_paged_attn(const hf_paged& c, PagedAttnArgs a, void* workspace, hipStream_t s);

@@ -9,8 +9,10 @@
 //   pieces  A sequence whose rows see w tiles at most is cut into ceil(w / C) parts of equal length, C = ceil(longest w / S); a workgroup
 //           takes a (key head, sequence, part, rows).  S is the best of 64 candidates, one a lane, by a model of the launch: with n = the
 //           work in row tiles as long as the longest and x = n S / compute units,
-//               rounds(x) (longest w / S * tile + start) + (S > 1 ? meet + join S : 0)  microseconds,
-//           rounds(x) = x rounded up where all rows see as much, else x + 3/4.  Only S with n S <= groups are looked at, and S = 1.
+//               rounds(x) (longest w / S * t(x) + start) + (S > 1 ? meet + join S : 0)  microseconds,
+//           rounds(x) = x rounded up where all rows see as much, else x + 3/4, and t(x) what a tile takes: `tile` where the compute units
+//           are full, and next to an idle half of them more (chunks) or, bound by memory, less (single tokens) than its share.  Only S with
+//           n S <= groups are looked at, and S = 1.
 //   shares  (few rows, where no two workgroups read the same keys) All row tiles of all key heads lie on one line, each as long as its
 //           key tiles (between a sequence's first and last row tile they are taken to grow evenly) and `lead` more for what its start
 //           costs; each of `groups` workgroups gets an equal share of the line.  A share's end that falls near a row tile's ends moves
@@ -34,7 +36,7 @@ struct PagedSchedule {
   int groups;                    // workgroups that may be parts of a row tile's work (32 rows: the grid, if there is work for so many)
   int lead;
   bool meets;                    // there is a workspace: 2 groups parts, and as many counters
-  float tile, tile_alone;        // microseconds a tile takes where the chip is full, and at least
+  float tile, tile_alone;        // microseconds a tile takes where the chip is full, and alone on a compute unit
   float start, meet, join;
   unsigned long long* counters;  // [2 groups] arrivals at a row tile
   float* parts;                  // [2 groups][BM][D], behind them [2 groups][BM][2]: row maximum and sum
@@ -70,21 +72,42 @@ __device__ __forceinline__ int thread_id() {
   return t;
 }
 
+// ---- pages, and tiles of keys.  A tile is 32 keys from a multiple of 32 on, or, page_tiles given, of a page: its last tile may be short
+__device__ __forceinline__ bool is_page(const PagedAttnArgs& a, int id) { return (unsigned)id < (unsigned)a.n_pages; }
+__device__ __forceinline__ int div_page(const PagedAttnArgs& a, int key) {   // key / a.page for 0 <= key < 2^31
+  return (int)(((unsigned long long)(unsigned)key * a.page_magic) >> a.page_shift);
+}
+__device__ __forceinline__ int div_tiles(const PagedAttnArgs& a, int tile) {
+  return (int)(((unsigned long long)(unsigned)tile * a.tiles_magic) >> a.tiles_shift);
+}
+__device__ __forceinline__ int tile_of(const PagedAttnArgs& a, int key) {   // that holds the key
+  if (a.page_tiles == 0) return key / kKeyTile;
+  const int page = div_page(a, key);
+  return page * a.page_tiles + (key - page * a.page) / kKeyTile;
+}
+__device__ __forceinline__ int tiles_to(const PagedAttnArgs& a, int key) { return key > 0 ? tile_of(a, key - 1) + 1 : 0; }   // that hold keys before it
+__device__ __forceinline__ int tile_start(const PagedAttnArgs& a, int tile) {
+  if (a.page_tiles == 0) return kKeyTile * tile;
+  const int page = div_tiles(a, tile);
+  return page * a.page + kKeyTile * (tile - page * a.page_tiles);
+}
+
 // the key tiles of some rows: 0 .. s1 - 1 (sink), then from s1 + skip on; n of them
 struct KeyTiles {
   int s1, skip, n;
-  __device__ __forceinline__ int start(int t) const { return kKeyTile * (t < s1 ? t : t + skip); }
+  __device__ __forceinline__ int tile(int t) const { return t < s1 ? t : t + skip; }
 };
 
 // tokens t_lo .. t_hi of a sequence with m new tokens and `len` in all, of which `held` can lie in the cache
 __device__ __forceinline__ KeyTiles key_tiles(const PagedAttnArgs& a, int m, int len, int held, int t_lo, int t_hi) {
   const int p_lo = len - m + t_lo, p_hi = len - m + t_hi;
   const int end = a.causal ? max(0, min(held, p_hi + 1)) : held;
-  const int w1 = (end + kKeyTile - 1) / kKeyTile;
+  const int w1 = tiles_to(a, end);
   KeyTiles k = {0, 0, w1};
   if (a.window > 0) {
-    const int w0 = (int)(max(0ll, (long long)p_lo - a.window + 1) / kKeyTile);
-    k.s1 = (min(a.n_sink, end) + kKeyTile - 1) / kKeyTile;
+    const long long first = (long long)p_lo - a.window + 1;
+    const int w0 = first <= 0 ? 0 : (first >= end ? w1 : tile_of(a, (int)first));
+    k.s1 = tiles_to(a, min(a.n_sink, end));
     k.skip = max(0, w0 - k.s1);
     k.n = min(k.s1, w1) + max(0, w1 - max(w0, k.s1));
   }
@@ -184,7 +207,9 @@ template <int BM, bool kShares> __device__ __forceinline__ PagedWork find_work(c
     const float S = lane < 32 ? (float)(lane + 1) : floorf(32.0f * __builtin_amdgcn_exp2f((float)(lane - 31) * (5.0f / 32.0f)));   // .. 1024
     const float x = n * S * (1.0f / kComputeUnits), full = fminf(x, 1.0f);
     const float rounds = x <= 1.0f ? 1.0f : (units > 0.98f * longest * rows ? ceilf(x) : x + 0.75f);
-    float cost = rounds * (longest / S * fmaxf(sc.tile_alone + 0.3f * sc.tile * full, sc.tile * full) + sc.start) + (lane > 0 ? sc.meet + sc.join * S : 0.0f);
+    const float work = kShares ? rounds * fmaxf(sc.tile_alone + 0.3f * sc.tile * full, sc.tile * full)
+                               : rounds * sc.tile + (rounds - 2.0f * floorf(0.5f * rounds)) * (sc.tile_alone - sc.tile);
+    float cost = longest / S * work + rounds * sc.start + (lane > 0 ? sc.meet + sc.join * S : 0.0f);
     if (lane > 0 && (most / longest * heads * S > (float)sc.groups || S > longest)) cost = INFINITY;
     const float best = -total_of(-cost, -INFINITY, larger);
     const int at = __ffsll(__ballot(cost == best)) - 1;
@@ -374,21 +399,14 @@ __device__ __forceinline__ RowView row_view(const PagedAttnArgs& a, const PagedI
   return v;
 }
 
-// ---- pages
-typedef const __attribute__((address_space(4))) int32_t* ScalarInts;   // read through the scalar unit: a uniform address, not written meanwhile
-
-__device__ __forceinline__ bool is_page(const PagedAttnArgs& a, int id) { return (unsigned)id < (unsigned)a.n_pages; }
-__device__ __forceinline__ int div_page(const PagedAttnArgs& a, int key) {   // key / a.page for 0 <= key < 2^31
-  return (int)(((unsigned long long)(unsigned)key * a.page_magic) >> a.page_shift);
-}
-// whether one of the item's entries is no page (uniform; every wavefront looks at all of them)
+// whether one of the item's entries is no page (uniform; every wavefront looks at all of them; tiles from multiples of 32 on)
 __device__ __forceinline__ bool any_bad_page(const PagedAttnArgs& a, const PagedItem& it) {
   if (it.t1 <= it.t0 || it.held == 0) return false;
   const int32_t* row = a.table + (long long)it.seq * a.max_pages;
   bool bad = false;
   auto scan = [&](int t0, int t1) {   // tiles t0 .. t1 - 1
-    const int last = div_page(a, min(it.keys.start(t1 - 1) + kKeyTile, it.held) - 1);
-    for (int e = div_page(a, it.keys.start(t0)) + (thread_id() & 63); e <= last; e += kWave) bad = bad || !is_page(a, row[e]);
+    const int last = div_page(a, min(kKeyTile * it.keys.tile(t1 - 1) + kKeyTile, it.held) - 1);
+    for (int e = div_page(a, kKeyTile * it.keys.tile(t0)) + (thread_id() & 63); e <= last; e += kWave) bad = bad || !is_page(a, row[e]);
   };
   if (it.t0 < it.keys.s1) scan(it.t0, min(it.t1, it.keys.s1));
   if (it.t1 > it.keys.s1) scan(max(it.t0, it.keys.s1), it.t1);

@@ -4,9 +4,10 @@
 //   S^T (keys x rows) = K_tile (A, from LDS) x Q^T (B, registers),   O^T (d x rows) += V_tile^T (A, LDS) x P^T (B, registers),
 // so that the statistics of a row are private to its two lanes and the exponentials of S^T are, rounded to bf16, the B operand of the
 // second product.  K and V tiles go global -> LDS directly, V^T fragments are transposing reads, three K slots and two V slots.
-// Here the rows are tokens x heads of a group, and a tile lies in pages.  A wavefront keeps 64 entries of the page table, a lane each; the
-// descriptor of a tile in one page is scalar arithmetic on one of them (read through the scalar unit instead, an entry is on its way when
-// the tile's barrier waits for everything that is: 12 heads x 4680 x 9360 0.33 ms).
+// Here the rows are tokens x heads of a group, and a tile lies in a page.  A wavefront finds out for 64 tiles at once where they lie, a lane
+// each; a tile's descriptor is then a few scalar instructions.  (12 heads x 4680 x 9360: 0.284 ms; with entries of the page table that the
+// scalar unit reads a tile ahead 0.33, they are on their way when the tile's barrier waits for everything that is; with tiles that go on in
+// the next page, and a branch for them, 0.311.)
 //
 // Three shapes of workgroup (NW wavefronts of rows, KS groups of wavefronts that share the keys):
 //   NW 8, KS 1   256 rows, tiles shared by eight wavefronts, one barrier a tile, one workgroup a compute unit (head_dim 128): long chunks
@@ -56,8 +57,8 @@ template <int D, int NW, int KS> struct Shape {
   static constexpr int LDS = KS * SPAN + (GROUP > OUT ? 0 : 16);
 };
 
-// kBig: pages in which tiles lie whole, or nearly all do (of a multiple of 32 tokens, or of 256 and more): one descriptor a tile, or, over two
-// pages, an address per lane.  Else every lane has an address: pages may end anywhere.
+// kBig: tiles end with their page: one descriptor a tile.  Else, where a page's last tile would be short too often, every lane has an address
+// and pages may end anywhere.
 template <int D, int NW, int KS, bool kBig>
 __global__ __launch_bounds__(64 * NW * KS, (NW > 1 ? 2 : 1)) void paged_attn_kernel(const PagedLaunch) {
   static_assert(NW == 1 || KS == 1, "groups share no barrier");
@@ -102,13 +103,13 @@ __global__ __launch_bounds__(64 * NW * KS, (NW > 1 ? 2 : 1)) void paged_attn_ker
 #pragma unroll
     for (int s = 0; s < NS; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(q + 16 * s);
   }
-  const bool bad_pages = any_bad_page(a, it);
+  const bool bad_pages = kBig ? false : any_bad_page(a, it);   // (kBig: such a tile has no bytes)
 
   // ---- the group's tiles, every wavefront of it the same: every KS-th of the item's, or (pages by lane) a run of them, whose pages are fewer
   constexpr int kStride = kBig ? KS : 1;
   const int run = (it.t1 - it.t0 + KS - 1) / KS, base_tile = it.t0 + grp * (kBig ? 1 : run);
   const int count = kBig ? max(0, (it.t1 - base_tile + KS - 1) / KS) : max(0, min(run, it.t1 - base_tile));
-  auto start_of = [&](int i) { return it.keys.start(base_tile + kStride * i); };   // (0 <= i < count)
+  auto start_of = [&](int i) { return tile_start(a, it.keys.tile(base_tile + kStride * i)); };   // (0 <= i < count)
 
   // ---- requests: 1 KB pieces; piece j of this wavefront is the tile's keys RPP (wave + NW j) ..  Keys that are none read as zeros
   const uint32_t page_rows = (uint32_t)a.heads_kv * (uint32_t)a.page, head_rows = (uint32_t)it.head_kv * (uint32_t)a.page;   // (of the pool: < 2^32)
@@ -137,39 +138,25 @@ __global__ __launch_bounds__(64 * NW * KS, (NW > 1 ? 2 : 1)) void paged_attn_ker
   };
   auto pool_row = [&](int id, int inside) { return (uint32_t)id * page_rows + head_rows + (uint32_t)inside; };
 
-  // kBig: where 64 tiles lie, a lane each: the pool's row of the first key, and how many bytes (-1: they go on in another page).  Of the
-  // tiles that K is requested for, and of those that V is, which come two later
+  // kBig: where 64 tiles lie, a lane each: the pool's row of the first key, and how many bytes.  Of the tiles that K is requested for, and of
+  // those that V is, which come two later
   struct Places { uint32_t row; int bytes; };
   Places k_places = {0, 0}, v_places = {0, 0};
   auto find_places = [&](int i0) {
     const int i = i0 + lane, start = i < count ? start_of(i) : it.held;
     k_places = {0, 0};
     if (start < it.held) {
-      const int entry = div_page(a, start), inside = start - entry * a.page, left = min(it.held - start, kKeyTile), id = table[entry];
+      const int entry = div_page(a, start), inside = start - entry * a.page, id = table[entry];
       k_places.row = pool_row(id, inside);
-      k_places.bytes = inside + left > a.page ? -1 : (is_page(a, id) ? left * ROWB : 0);
+      k_places.bytes = is_page(a, id) ? min(min(it.held - start, a.page - inside), kKeyTile) * ROWB : 0;
     }
   };
-  auto request_big = [&](uint64_t pool, const Places& p, int i, uint32_t slot, const int (&off)[CPT]) {
+  auto request_big = [&](uint64_t pool, const Places& p, int i, uint32_t slot, const int (&off)[CPT]) {   // its bytes
     const int bytes = __builtin_amdgcn_readlane(p.bytes, i & 63);
-    const uint32_t row = __builtin_amdgcn_readlane(p.row, i & 63);
-    const uint64_t base = pool + (uint64_t)row * ROWB;
-    if (bytes >= 0) {   // (uniform)
+    const uint64_t base = pool + (uint64_t)(uint32_t)__builtin_amdgcn_readlane(p.row, i & 63) * ROWB;
 #pragma unroll
-      for (int j = 0; j < CPT; ++j) to_lds(slot + (wave + NW * j) * 1024, off[j], base, bytes);
-    } else {            // two pages: an address per lane
-      const ScalarInts entries = (ScalarInts)table;
-      int start = start_of(i);
-      asm volatile("" : "+s"(start));   // (what follows stays behind the branch)
-      const int entry = div_page(a, start), cut = (entry + 1) * a.page - start, id0 = entries[entry], id1 = entries[entry + 1];
-      const uint64_t next = pool + (uint64_t)pool_row(id1, 0) * ROWB - (uint64_t)(uint32_t)(cut * ROWB);
-#pragma unroll
-      for (int j = 0; j < CPT; ++j) {
-        const int r = RPP * (wave + NW * j) + lane / UPR;
-        const bool ok = start + r < it.held && is_page(a, r < cut ? id0 : id1);
-        to_lds_from(slot + (wave + NW * j) * 1024, ok ? (r < cut ? base : next) + (uint32_t)off[j] : zeros);
-      }
-    }
+    for (int j = 0; j < CPT; ++j) to_lds(slot + (wave + NW * j) * 1024, off[j], base, bytes);
+    return bytes;
   };
   // else: the pool's row of the lane's key (the tile's key lane % 32), kNoRow: none; of tiles i + 1 .. i + 3.  The wavefront keeps 64 entries
   // of the table, from ids_base on, a lane each
@@ -196,10 +183,11 @@ __global__ __launch_bounds__(64 * NW * KS, (NW > 1 ? 2 : 1)) void paged_attn_ker
     }
   };
   // V of tile i + 1 and K of tile i + 3, whose turn it is in step i
+  int bytes_next = 0;   // kBig: of the tile whose V was requested last
   auto request_v = [&](int i, uint32_t slot) {
     if constexpr (kBig) {
       if (((i + 1) & 63) == 0) v_places = k_places;
-      request_big(v_pool, v_places, i + 1, slot, v_off);
+      bytes_next = request_big(v_pool, v_places, i + 1, slot, v_off);
     } else {
       request_rows(v_pool, row1, slot, v_off);
     }
@@ -240,17 +228,18 @@ __global__ __launch_bounds__(64 * NW * KS, (NW > 1 ? 2 : 1)) void paged_attn_ker
   bool odd = false;   // values that are not finite lie next to rows that do not see them: they were left out (uniform)
 
   // the tiles of which every row of the wavefront sees all keys (uniform): i_all .. i_all + n_all - 1, behind the sink's
-  auto first_from = [&](int key) {   // the first i whose tile lies behind the sink's and starts at `key` or behind
-    const int t = max(it.keys.s1, (key + kKeyTile - 1) / kKeyTile - it.keys.skip) - base_tile;
+  auto index_of = [&](int tile) {   // the first i at that tile (of those behind the sink's) or behind it
+    const int t = max(it.keys.s1, tile - it.keys.skip) - base_tile;
     return t <= 0 ? 0 : (t + kStride - 1) / kStride;
   };
-  const int i_all = first_from(view_hi.lo), n_all = bad_pages ? 0 : max(0, first_from(view_lo.hi - (kKeyTile - 1)) - i_all);
+  const int i_all = index_of(tiles_to(a, view_hi.lo)), n_all = bad_pages ? 0 : max(0, index_of(tile_of(a, view_lo.hi)) - i_all);
   auto all_of = [&](int i) { return (unsigned)(i - i_all) < (unsigned)n_all; };
-  // the tile's keys that lie in pages, a bit each
-  auto existing = [&](int start) {
+  // the tile's keys that are there, a bit each
+  auto existing = [&](int start, int bytes) {
+    if constexpr (kBig) return RowView::below(bytes / ROWB);
     if (!bad_pages) return 0xffffffffu;
     const int key = start + l32;
-    return (uint32_t)__ballot(key < it.held && is_page(a, a.table[(long long)it.seq * a.max_pages + div_page(a, min(key, key_last))]));
+    return (uint32_t)__ballot(key < it.held && is_page(a, table[div_page(a, min(key, key_last))]));
   };
 
   // the rows have to be here before the first request: the compiler does not count requests, and a wait behind them would be one for
@@ -262,7 +251,7 @@ __global__ __launch_bounds__(64 * NW * KS, (NW > 1 ? 2 : 1)) void paged_attn_ker
       find_places(0);
       v_places = k_places;
       request_big(k_pool, k_places, 0, sK_lds, k_off);
-      request_big(v_pool, k_places, 0, sV_lds, v_off);
+      bytes_next = request_big(v_pool, k_places, 0, sV_lds, v_off);
       request_big(k_pool, k_places, 1, sK_lds + TILE, k_off);
       request_big(k_pool, k_places, 2, sK_lds + 2 * TILE, k_off);
     } else {
@@ -284,6 +273,7 @@ __global__ __launch_bounds__(64 * NW * KS, (NW > 1 ? 2 : 1)) void paged_attn_ker
 
   // tile i: its K fragments are in registers; slot_next, slot_new: where K of tiles i + 1 and i + 3 lie; par: V slot of tile i
   auto step = [&](int i, const int slot_next, const int slot_new, const int par) {
+    const int bytes = bytes_next;
     f32x16 sacc;
 #pragma unroll
     for (int r = 0; r < 16; ++r) sacc[r] = 0.0f;
@@ -308,9 +298,9 @@ __global__ __launch_bounds__(64 * NW * KS, (NW > 1 ? 2 : 1)) void paged_attn_ker
     for (int s = 0; s < NS; ++s) kf[s] = *reinterpret_cast<const bf16x8*>(sK + k_addr[s] + slot_next * TILE);
     __builtin_amdgcn_sched_barrier(0);
     {
-      if (!all_of(i)) {
+      if (!all_of(i) || (kBig && bytes < TILE)) {
         const int start = start_of(i);
-        const uint32_t sees = view.sees_tile(start) & existing(start), mine = sees >> (4 * h);
+        const uint32_t sees = view.sees_tile(start) & existing(start, bytes), mine = sees >> (4 * h);
         seen |= sees;
 #pragma unroll
         for (int r = 0; r < 16; ++r) sacc[r] = masked_score(sacc[r], mine, 8 * (r >> 2) + (r & 3));
@@ -408,12 +398,10 @@ __global__ __launch_bounds__(64 * NW * KS, (NW > 1 ? 2 : 1)) void paged_attn_ker
     const float m_use = m_ref == -INFINITY ? 0.0f : m_ref;
 #pragma unroll 1
     for (int i = 0; i < count; ++i) {
-      if (all_of(i)) continue;
-      const int start = start_of(i);
+      const int start = start_of(i), tile_end = kBig ? min(start + kKeyTile, (div_page(a, start) + 1) * a.page) : start + kKeyTile;
+      if (all_of(i) && tile_end == start + kKeyTile) continue;
 #pragma unroll 1
-      for (int k = 0; k < kKeyTile; ++k) {
-        const int key = start + k;
-        if (key >= it.held) break;
+      for (int key = start; key < min(tile_end, it.held); ++key) {
         const int entry = div_page(a, key), id = table[entry];
         if (!is_page(a, id)) continue;
         const uint64_t at = (uint64_t)pool_row(id, key - entry * a.page) * ROWB;
@@ -491,17 +479,25 @@ Plan plan_of(const hf_paged& c, int n_q) {
   } else {
     p.sc.groups = 131072 / p.rows / 2;
     p.sc.tile = p.rows == 256 ? 0.89f : 0.535f;
-    p.sc.tile_alone = 0.7f * p.sc.tile;
+    p.sc.tile_alone = p.rows == 256 ? 0.89f : 0.7f;
     p.sc.start = p.rows == 256 ? 9.0f : 5.0f;
     p.sc.meet = 6.0f;
     p.sc.join = 1.0f;
   }
-  const long long key_tiles = ((long long)c.max_pages * c.page_tokens + kKeyTile - 1) / kKeyTile;   // (at most)
+  const long long key_tiles = (long long)c.max_pages * ((c.page_tokens + kKeyTile - 1) / kKeyTile);   // (at most)
   long long grid = p.rows == 32 ? p.sc.groups : tiles(p.rows) + p.sc.groups;
   if (grid > tiles(p.rows) * key_tiles) grid = tiles(p.rows) * key_tiles;
   p.grid = (int)((grid + 7) & ~7ll);
   p.sc.meets = key_tiles > 1;
   return p;
+}
+
+// n / d = n * magic >> shift (the result) for n < 2^31
+int magic_of(int d, uint32_t& magic) {
+  int bits = 0;
+  while ((1 << bits) < d) ++bits;
+  magic = (uint32_t)((1ull << (31 + bits)) / (unsigned)d + 1);
+  return 31 + bits;
 }
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -516,7 +512,7 @@ template <int D, int NW, int KS, bool kBig> int launch(const PagedAttnArgs& a, c
 }
 
 template <int D> int launch_of(const PagedAttnArgs& a, const PagedSchedule& sc, const Plan& p, hipStream_t s) {
-  const bool big = a.page % kKeyTile == 0 || a.page >= 256;
+  const bool big = a.page_tiles > 0;
   if constexpr (D == 128) {
     if (p.rows == 256) return big ? launch<D, 8, 1, true>(a, sc, p.grid, s) : launch<D, 8, 1, false>(a, sc, p.grid, s);
   }
@@ -535,15 +531,18 @@ size_t paged_workspace_bytes(const hf_paged& c, int n_q) {
 
 int launch_paged_attn(const hf_paged& c, PagedAttnArgs a, void* workspace, hipStream_t s) {
   const Plan p = plan_of(c, a.n_q);
-  int shift = 0;
-  while ((1 << shift) < c.page_tokens) ++shift;
-  a.page_shift = 31 + shift;
-  a.page_magic = (uint32_t)((1ull << a.page_shift) / (unsigned)c.page_tokens + 1);
+  a.page_shift = magic_of(c.page_tokens, a.page_magic);
   PagedSchedule sc = p.sc;
   if (sc.meets) {
     sc.counters = static_cast<unsigned long long*>(workspace);
     sc.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + align256((size_t)sc.groups * 16));
     sc.tag = next_call_tag();
+  }
+  // tiles that end with their page where the last, short ones are a sixteenth at most
+  const int tiles = (c.page_tokens + kKeyTile - 1) / kKeyTile;
+  if (c.dtype == HF_BF16 && tiles * kKeyTile * 16 <= c.page_tokens * 17) {
+    a.page_tiles = tiles;
+    a.tiles_shift = magic_of(tiles, a.tiles_magic);
   }
   if (c.dtype == HF_F32) return launch_paged_attn_f32(c, a, sc, p.rows, p.grid, s);
   return c.head_dim == 128 ? launch_of<128>(a, sc, p, s) : launch_of<64>(a, sc, p, s);

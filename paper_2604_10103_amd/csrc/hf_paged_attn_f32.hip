@@ -66,7 +66,7 @@ __global__ __launch_bounds__(64 * NW * KS, 1) void paged_attn_f32_kernel(const P
 
   const bool bad_pages = any_bad_page(a, it);
   const int count = active ? max(0, (it.t1 - it.t0 - grp + KS - 1) / KS) : 0;
-  auto start_of = [&](int i) { return it.keys.start(it.t0 + grp + KS * i); };
+  auto start_of = [&](int i) { return kKeyTile * it.keys.tile(it.t0 + grp + KS * i); };   // (page_tiles = 0)
   auto some_of = [&](int start) { return start < view_hi.hi && (start + kKeyTile > view_lo.lo || start < view.sink); };
   auto all_of = [&](int start) {
     return start + kKeyTile <= view_lo.hi && (start >= view_hi.lo || start + kKeyTile <= view.sink) && !bad_pages;

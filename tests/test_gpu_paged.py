@@ -104,6 +104,28 @@ def test_pages_of_any_size(dtype, page):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("page", [94, 256, 300, 500, 1000])
+@pytest.mark.parametrize("mask", [dict(), dict(causal=False, window=400, n_sink=70), dict(window=333, n_sink=95)])
+def test_long_pages_end_inside_a_tile(dtype, page, mask):
+    b = Batch([1, 290, 2], [1300, 1290, 501], 4, 2, 128, dtype, page, seed=page, **mask)
+    b.check(*b.attend())
+    b = Batch([1, 3], [1300, 999], 4, 1, 64, dtype, page, seed=page, **mask)
+    b.check(*b.attend())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("page", [16, 64, 94])
+def test_pages_that_are_none_inside_long_contexts(dtype, page):
+    b = Batch([1, 200, 40], [1300, 700, 41], 4, 2, 128, dtype, page, seed=page)
+    b.table[0, 3] = b.table[0, 5] = -5
+    b.table[1, 2] = b.n_pages
+    b.table[1, 5] = 2 ** 31 - 1
+    b.table[2, 0] = -1
+    b.to_gpu()
+    b.check(*b.attend())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("heads,heads_kv", [(1, 1), (3, 3), (5, 1), (16, 1), (33, 1), (70, 2), (40, 8), (12, 12)])
 def test_groups_of_heads(dtype, heads, heads_kv):
     b = Batch([1, 2, 9], [40, 100, 9], heads, heads_kv, 64, dtype, 16, seed=heads)
@@ -152,19 +174,20 @@ def test_rows_without_a_key(dtype):
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
 @pytest.mark.parametrize("mask", [dict(), dict(window=20, n_sink=4), dict(causal=False)])
 @pytest.mark.parametrize("new,n", [(70, 70), (150, 200), (3, 90), (1, 64)])
-def test_what_is_not_seen_does_not_count(dtype, d, bad, mask, new, n):
+@pytest.mark.parametrize("page", [24, 64, 94])
+def test_what_is_not_seen_does_not_count(dtype, d, bad, mask, new, n, page):
     """Keys and values that are not finite reach the rows that see them and no others, beyond the length included."""
-    b = Batch([new, 1], [n, 50], 4, 2, d, dtype, 24, seed=12, **mask)
+    b = Batch([new, 1], [n, 50], 4, 2, d, dtype, page, seed=12, **mask)
     b.check(*b.attend())
     ref = b.oracle()
     clean, clean_lse = b.attend()
     where = [j for j in {n - 1, n - new + new // 2, n - new // 3, max(0, n - 40)} if 0 <= j < n]
     for pages in (b.K_pages, b.V_pages):
         for j in where:
-            pages[int(b.table[0, j // 24]), :, j % 24, :5] = bad
+            pages[int(b.table[0, j // page]), :, j % page, :5] = bad
         for s, length in ((0, n), (1, 50)):                    # what lies behind the length in its last page
-            if length % 24:
-                pages[int(b.table[s, length // 24]), :, length % 24:] = bad
+            if length % page:
+                pages[int(b.table[s, length // page]), :, length % page:] = bad
         for spare in set(range(b.n_pages)) - set(b.table.flatten().tolist()):
             pages[spare] = bad
     O, lse = b.attend()
@@ -185,14 +208,15 @@ def test_what_is_not_seen_does_not_count(dtype, d, bad, mask, new, n):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
-def test_values_that_are_not_finite_reach_their_features(dtype, d, bad):
+@pytest.mark.parametrize("page", [24, 32, 94])
+def test_values_that_are_not_finite_reach_their_features(dtype, d, bad, page):
     """Values alone: a visible one makes its own feature NaN or that infinity, the others stay within their bounds."""
     new, n = 100, 140
-    b = Batch([new], [n], 4, 2, d, dtype, 24, window=50, n_sink=2, seed=13)
+    b = Batch([new], [n], 4, 2, d, dtype, page, window=50, n_sink=2, seed=13)
     ref = b.oracle()
     where = {90: 3, 120: d - 1, 139: 17, 45: 40}
     for j, f in where.items():
-        b.V_pages[int(b.table[0, j // 24]), :, j % 24, f] = bad
+        b.V_pages[int(b.table[0, j // page]), :, j % page, f] = bad
     O, lse = b.attend()
     got, fine = f64(O), np.ones((new, d), dtype=bool)
     for i in range(new):
