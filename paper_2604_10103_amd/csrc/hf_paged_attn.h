@@ -6,12 +6,12 @@
 // Work.  The grid is fixed by what the host knows; what a workgroup does follows from the lengths, which only the device knows: every
 // wavefront derives it for itself from cu_new and seq_lens, 64 sequences at a time, without exchange.  Keys count in tiles of 32.
 //
-//   pieces  A sequence whose rows see w tiles at most is cut into ceil(w / C) parts of equal length, C = ceil(longest w / S); a workgroup
-//           takes a (key head, sequence, part, rows).  S is the best of 64 candidates, one a lane, by a model of the launch: with n = the
+//   pieces  A row tile that sees w tiles is cut into ceil(w / C) parts of equal length, C = ceil(longest w / S); a workgroup takes a (key
+//           head, sequence, part, rows).  S is the best of 64 candidates, one a lane, by a model of the launch: with n = the
 //           work in row tiles as long as the longest and x = n S / compute units,
 //               rounds(x) (longest w / S * t(x) + start) + (S > 1 ? meet + join S : 0)  microseconds,
-//           rounds(x) = x rounded up where all rows see as much, else x + 3/4, and t(x) what a tile takes: `tile` where the compute units
-//           are full, and next to an idle half of them more (chunks) or, bound by memory, less (single tokens) than its share.  Only S with
+//           rounds(x) = x rounded up where all pieces are as long, else x + 1/2 (single tokens: 3/4), and t(x) what a tile takes: `tile` where
+//           the compute units are full, and next to an idle half of them more (chunks) or, bound by memory, less (single tokens) than its share.  Only S with
 //           n S <= groups are looked at, and S = 1.
 //   shares  (few rows, where no two workgroups read the same keys) All row tiles of all key heads lie on one line, each as long as its
 //           key tiles (between a sequence's first and last row tile they are taken to grow evenly) and `lead` more for what its start
@@ -177,6 +177,22 @@ struct PagedWork {
 };
 
 constexpr float kComputeUnits = 256;
+
+// pieces of C tiles: a sequence's parts lie in layers.  Row tile r is in layer p < layers() if it sees more than p C tiles, and so has as many
+// parts as layers that hold it; new tokens see more the later they are, so that layer p holds the row tiles from first_row(p) on
+__device__ __forceinline__ int layers(const SeqWork& q, int C) { return (max(q.v0, q.v1) + C - 1) / C; }
+template <int BM> __device__ __forceinline__ int first_row(const PagedAttnArgs& a, const SeqWork& q, int C, int p) {
+  if (!a.causal || p * C < q.v0) return 0;
+  const int token = min(max(tile_start(a, p * C) - (q.len - q.m), 0), max(q.m - 1, 0));
+  return min(token * (a.heads / a.heads_kv) / BM, max(q.T - 1, 0));
+}
+template <int BM> __device__ __forceinline__ int pieces_of(const PagedAttnArgs& a, const SeqWork& q, int C) {
+  const int S = layers(q, C), all = a.causal && q.T > 1 ? min(S, (q.v0 + C - 1) / C) : S;
+  int n = all * q.T;
+  for (int p = all; p < S; ++p) n += q.T - first_row<BM>(a, q, C, p);
+  return n;
+}
+
 constexpr int kNear = 4;     // a share ends at a row tile's end, or at least this many tiles from it
 
 template <int BM> __device__ __forceinline__ int line_at(const SeqWork& q, int r, int lead) {   // where row tile r of a sequence lies
@@ -188,29 +204,31 @@ template <int BM, bool kShares> __device__ __forceinline__ PagedWork find_work(c
   const int lane = thread_id() & 63;
   const auto add = [](float x, float y) { return x + y; };
   const auto larger = [](float x, float y) { return fmaxf(x, y); };
-  float units = 0.0f, most = 0.0f, rows = 0.0f, longest = 1.0f;
+  float units = 0.0f, rows = 0.0f, longest = 1.0f;
   SeqWork q;
   for (int s0 = 0; s0 < a.n_seqs; s0 += kWave) {
     q = seq_work<BM>(a, s0 + lane);
-    units += (float)q.T * 0.5f * (float)(q.v0 + q.v1);
-    most += (float)q.T * (float)max(q.v0, q.v1);
-    rows += (float)q.T;
+    // from row tile to row tile what they see grows by their tokens until it is v1 (shrinks, where a window ends and nothing is causal)
+    const float v0 = (float)q.v0, v1 = (float)q.v1, T = (float)q.T;
+    const float grows = fminf(T, fabsf(v1 - v0) * (float)(kKeyTile * (a.heads / a.heads_kv)) * (1.0f / BM));
+    units += T * v1 + 0.5f * grows * (v0 - v1);
+    rows += T;
     longest = fmaxf(longest, (float)(q.T > 0 ? max(q.v0, q.v1) : 1));
   }
   PagedWork p = {false, 0x3fffffff, 0, 0, 0, 1};
   if (sc.meets) {
     units = total_of(units, 0.0f, add);
-    most = total_of(most, 0.0f, add);
     rows = total_of(rows, 0.0f, add);
     longest = total_of(longest, 0.0f, larger);
     const float heads = (float)a.heads_kv, n = units / longest * heads;
     const float S = lane < 32 ? (float)(lane + 1) : floorf(32.0f * __builtin_amdgcn_exp2f((float)(lane - 31) * (5.0f / 32.0f)));   // .. 1024
     const float x = n * S * (1.0f / kComputeUnits), full = fminf(x, 1.0f);
-    const float rounds = x <= 1.0f ? 1.0f : (units > 0.98f * longest * rows ? ceilf(x) : x + 0.75f);
+    const bool alike = units > 0.98f * longest * rows || (!kShares && lane > 0);
+    const float rounds = x <= 1.0f ? 1.0f : (alike ? ceilf(x) : x + (kShares ? 0.75f : 0.5f));
     const float work = kShares ? rounds * fmaxf(sc.tile_alone + 0.3f * sc.tile * full, sc.tile * full)
                                : rounds * sc.tile + (rounds - 2.0f * floorf(0.5f * rounds)) * (sc.tile_alone - sc.tile);
     float cost = longest / S * work + rounds * sc.start + (lane > 0 ? sc.meet + sc.join * S : 0.0f);
-    if (lane > 0 && (most / longest * heads * S > (float)sc.groups || S > longest)) cost = INFINITY;
+    if (lane > 0 && (n * S > (float)sc.groups || S > longest)) cost = INFINITY;
     const float best = -total_of(-cost, -INFINITY, larger);
     const int at = __ffsll(__ballot(cost == best)) - 1;
     const float s_best = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(S), at));
@@ -223,15 +241,21 @@ template <int BM, bool kShares> __device__ __forceinline__ PagedWork find_work(c
   }
   p.C = __builtin_amdgcn_readfirstlane(p.C);
   p.shares = kShares && __builtin_amdgcn_readfirstlane((int)p.shares);
-  for (int s0 = 0; s0 < a.n_seqs; s0 += kWave) {
-    if (a.n_seqs > kWave) q = seq_work<BM>(a, s0 + lane);
-    if (p.shares) {
-      p.line += total_sum(line_at<BM>(q, q.T, sc.lead));
-    } else {
-      const int S = (max(q.v0, q.v1) + p.C - 1) / p.C;
-      p.each += total_sum(q.T * S);
-      p.split_each += total_sum(S > 1 ? q.T * S : 0);
+  for (bool once = true;; once = false) {
+    p.each = p.split_each = p.line = 0;
+    for (int s0 = 0; s0 < a.n_seqs; s0 += kWave) {
+      if (a.n_seqs > kWave) q = seq_work<BM>(a, s0 + lane);
+      if (p.shares) {
+        p.line += total_sum(line_at<BM>(q, q.T, sc.lead));
+      } else {
+        const int e = pieces_of<BM>(a, q, p.C);
+        p.each += total_sum(e);
+        p.split_each += total_sum(layers(q, p.C) > 1 ? e : 0);
+      }
     }
+    // more than there is room for, which an estimate may come to: nothing is cut
+    if (p.shares || !once || (p.split_each * a.heads_kv <= 2 * sc.groups && (kShares || p.each * a.heads_kv <= (int)gridDim.x))) break;
+    p.C = 0x3fffffff;
   }
   if (p.shares) p.share = max((int)(((long long)p.line * a.heads_kv + sc.groups - 1) / sc.groups), sc.lead + 3 * kNear);
   return p;
@@ -276,25 +300,48 @@ template <int BM> __device__ __forceinline__ void set_rows(const PagedAttnArgs& 
 
 // pieces: the `item`-th
 template <int BM> __device__ __forceinline__ bool find_piece(const PagedAttnArgs& a, const PagedSchedule& sc, const PagedWork& p, int item, PagedItem& it) {
-  if (item >= p.each * a.heads_kv || p.split_each * a.heads_kv > 2 * sc.groups) return false;   // (the latter cannot be)
+  if (item >= p.each * a.heads_kv) return false;
   it.head_kv = item / p.each;
-  const int y = item - it.head_kv * p.each;
-  auto parts = [&](const SeqWork& q) { return (max(q.v0, q.v1) + p.C - 1) / p.C; };
+  const int y = item - it.head_kv * p.each, lane = thread_id() & 63;
   SeqWork q;
   int seq, before, split_before;
   if (!find_seq<BM>(a, y, [&](const SeqWork& x, int& split) {
-        const int S = parts(x);
-        split = S > 1 ? x.T * S : 0;
-        return x.T * S;
+        const int e = pieces_of<BM>(a, x, p.C);
+        split = layers(x, p.C) > 1 ? e : 0;
+        return e;
       }, q, seq, before, split_before)) return false;
-  // within a sequence: part, then rows, the last ones (which see most) first
-  const int idx = y - before, back = idx % q.T;
-  it.part = idx / q.T;
-  it.parts = parts(q);
+  // within a sequence: layer, then rows, the last ones (which see most) first.  A row tile's parts have consecutive places in the workspace
+  const int S = layers(q, p.C), idx = y - before;
+  int back, at = 0;   // at: parts of the row tiles behind this one
+  if (!a.causal || q.T == 1 || S == 1) {
+    it.part = idx / q.T;
+    it.parts = S;
+    back = idx - it.part * q.T;
+    at = back * S;
+  } else {
+    int done = 0;
+    back = it.part = it.parts = 0;
+    for (int p0 = 0; p0 < S; p0 += kWave) {
+      const int e = p0 + lane < S ? q.T - first_row<BM>(a, q, p.C, p0 + lane) : 0, upto = done + scan_sum(e);
+      const unsigned long long owner = __ballot(idx >= upto - e && idx < upto);
+      if (owner) {
+        const int src = __ffsll(owner) - 1;
+        it.part = p0 + src;
+        back = idx - __builtin_amdgcn_readlane(upto - e, src);
+        break;
+      }
+      done = __builtin_amdgcn_readlane(upto, 63);
+    }
+    for (int p0 = 0; p0 < S; p0 += kWave) {
+      const int e = p0 + lane < S ? q.T - first_row<BM>(a, q, p.C, p0 + lane) : 0;
+      it.parts += __popcll(__ballot(back < e));
+      at += total_sum(min(back, e));
+    }
+  }
   set_rows<BM>(a, q, seq, q.T - 1 - back, it);
-  it.counter = it.slot0 = it.head_kv * p.split_each + split_before + back;   // (meant where there are parts)
-  it.slot1 = it.slot0 + q.T;
-  it.slot_step = q.T;
+  it.counter = it.slot0 = it.head_kv * p.split_each + split_before + at;   // (meant where there are parts)
+  it.slot1 = it.slot0 + 1;
+  it.slot_step = 1;
   it.t0 = (int)((long long)it.keys.n * it.part / it.parts);
   it.t1 = (int)((long long)it.keys.n * (it.part + 1) / it.parts);
   return true;

@@ -477,12 +477,22 @@ Plan plan_of(const hf_paged& c, int n_q) {
     p.sc.join = 0.1f;
     p.sc.lead = 5;
   } else {
+    const bool wide = c.head_dim == 128;
     p.sc.groups = 131072 / p.rows / 2;
-    p.sc.tile = p.rows == 256 ? 0.89f : 0.535f;
-    p.sc.tile_alone = p.rows == 256 ? 0.89f : 0.7f;
-    p.sc.start = p.rows == 256 ? 9.0f : 5.0f;
     p.sc.meet = 6.0f;
     p.sc.join = 1.0f;
+    p.sc.start = 5.0f;
+    if (c.dtype == HF_F32) {
+      p.sc.tile = wide ? 4.35f : 2.35f;
+      p.sc.tile_alone = wide ? 4.66f : 2.9f;
+      p.sc.start = 9.0f;
+    } else if (p.rows == 256) {
+      p.sc.tile = p.sc.tile_alone = 0.89f;
+      p.sc.start = 9.0f;
+    } else {
+      p.sc.tile = wide ? 0.535f : 0.29f;
+      p.sc.tile_alone = wide ? 0.7f : 0.4f;
+    }
   }
   const long long key_tiles = (long long)c.max_pages * ((c.page_tokens + kKeyTile - 1) / kKeyTile);   // (at most)
   long long grid = p.rows == 32 ? p.sc.groups : tiles(p.rows) + p.sc.groups;

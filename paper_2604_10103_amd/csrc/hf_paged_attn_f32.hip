@@ -1,9 +1,12 @@
 // Attention over a cache of pages in fp32 (hf_paged_attn_fwd, fp32 storage): both products on v_mfma_f32_32x32x2_f32.
 //
-// Rows, items and statistics as in hf_paged_attn.hip (the instruction's result has the same layout).  Nothing passes through LDS before
-// the end: a lane reads its key's row in 16-byte pieces (product over features), and of every value row the 16 or 8 bytes whose features
-// are its operands (product over keys), each row by an address of its own, so that pages may end anywhere; a key that is none reads a
-// row of zeros.  The four k indices of a piece feed four instructions; accumulator e holds the features E * (row of the result) + e.
+// Rows, items and statistics as in hf_paged_attn.hip (the instruction's result has the same layout).  A lane's operands are 16-byte pieces of
+// its key's row (product over features), and of every value row the 16 or 8 bytes that hold its features (product over keys).  The four k
+// indices of a piece feed four instructions; accumulator e holds the features E * (row of the result) + e.  Every key has an address of its
+// own, so that pages may end anywhere; a key that is none reads a row of zeros.
+//   NW 4, KS 1   128 rows, tiles of 32 keys go global -> LDS directly, a tile ahead, one barrier each; two workgroups or more a compute unit
+//                keep its matrix cores busy while one of them is at its exponentials
+//   NW 1, KS 4   32 rows, bound by memory: every wavefront reads its own tiles from memory to registers
 #include "hf_paged_attn.h"
 
 namespace hf {
@@ -19,8 +22,10 @@ __device__ float zero_row_f32[128];
 __device__ __forceinline__ bool not_finite(float v) { return (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u; }
 
 template <int D, int NW, int KS>
-__global__ __launch_bounds__(64 * NW * KS, 1) void paged_attn_f32_kernel(const PagedLaunch) {
-  constexpr int BM = 32 * NW, NT = 64 * NW * KS, NC = D / 8, E = D / 32;   // 16-byte pieces of a key; features of a lane's piece of a value
+__global__ __launch_bounds__(64 * NW * KS, NW > 1 ? 2 : 1) void paged_attn_f32_kernel(const PagedLaunch) {
+  static_assert(NW == 1 || KS == 1, "groups share no barrier");
+  constexpr int BM = 32 * NW, NT = 64 * NW * KS, NC = D / 8, E = D / 32;   // a lane's pieces of a key; features of its piece of a value
+  constexpr int ROWB = 4 * D, TILE = kKeyTile * ROWB, RPP = 1024 / ROWB, UPR = ROWB / 16;   // (LDS: keys of a 1 KB request, 16-byte units of a key)
   constexpr int SPAN = BM * (D + 4) + BM * 2;                              // a group's sums and statistics, in floats
   extern __shared__ __attribute__((aligned(16))) float sums[];
   typedef float piece __attribute__((ext_vector_type(E)));
@@ -65,7 +70,7 @@ __global__ __launch_bounds__(64 * NW * KS, 1) void paged_attn_f32_kernel(const P
   uint32_t seen = 0;
 
   const bool bad_pages = any_bad_page(a, it);
-  const int count = active ? max(0, (it.t1 - it.t0 - grp + KS - 1) / KS) : 0;
+  const int count = active || NW > 1 ? max(0, (it.t1 - it.t0 - grp + KS - 1) / KS) : 0;
   auto start_of = [&](int i) { return kKeyTile * it.keys.tile(it.t0 + grp + KS * i); };   // (page_tiles = 0)
   auto some_of = [&](int start) { return start < view_hi.hi && (start + kKeyTile > view_lo.lo || start < view.sink); };
   auto all_of = [&](int start) {
@@ -83,17 +88,42 @@ __global__ __launch_bounds__(64 * NW * KS, 1) void paged_attn_f32_kernel(const P
     const int key = start_of(i) + l32;
     return (id * page_rows + head_row + (key - div_page(a, key) * a.page)) * D;
   };
+  // ---- NW 1: registers
   auto load_keys = [&](f32x4 (&k)[NC], int i, int id) {
     const uintptr_t p = reinterpret_cast<uintptr_t>((id >= 0 ? static_cast<const float*>(a.K_pages) + offset_of(i, id) : zero_row_f32) + 4 * h);
 #pragma unroll
     for (int c = 0; c < NC; ++c) k[c] = *(const HF_GLOBAL f32x4*)(p + 32 * c);
   };
+  // ---- NW 4: two slots of a K and a V tile; unit u of key row r sits at u ^ r (modulo the row) in K, so that 8 lanes read 8 places
+  typedef __attribute__((address_space(3))) char* Lds;
+  const uint32_t lds = (uint32_t)(uintptr_t)(Lds)(char*)sums;
+  auto request = [&](int i, int id) {
+    const long long at = id >= 0 ? offset_of(i, id) * 4 : -1;
+    const uint32_t slot = lds + (i & 1) * 2 * TILE;
+#pragma unroll
+    for (int j = 0; j < kKeyTile / RPP / NW; ++j) {
+      const int piece_at = wave + NW * j, r = RPP * piece_at + lane / UPR, u = lane % UPR;
+      const long long row = __shfl(at, r, kWave);
+      const uint64_t zeros = reinterpret_cast<uint64_t>(zero_row_f32);
+      const uint64_t k = row >= 0 ? reinterpret_cast<uint64_t>(a.K_pages) + row + 16 * (u ^ (r % UPR)) : zeros;
+      const uint64_t v = row >= 0 ? reinterpret_cast<uint64_t>(a.V_pages) + row + 16 * u : zeros;
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                   :: "s"(__builtin_amdgcn_readfirstlane(slot + 1024 * piece_at)), "v"(k) : "memory", "m0");
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                   :: "s"(__builtin_amdgcn_readfirstlane(slot + TILE + 1024 * piece_at)), "v"(v) : "memory", "m0");
+    }
+  };
+  if constexpr (NW > 1) {   // the rows have to be here before the first request, which the compiler does not count: a wait behind it would be
+#pragma unroll              // one for it as well
+    for (int c = 0; c < NC; ++c) asm volatile("" : "+v"(qf[c]));
+  }
   int id = -1, id_next = -1;
   f32x4 kf[NC];
   if (count > 0) {
     id = page_of(0);
     id_next = page_of(1);
-    load_keys(kf, 0, id);
+    if constexpr (NW > 1) request(0, id);
+    else load_keys(kf, 0, id);
   }
   bool odd = false;   // values that are not finite lie next to rows that do not see them: they were left out (uniform)
 
@@ -101,29 +131,23 @@ __global__ __launch_bounds__(64 * NW * KS, 1) void paged_attn_f32_kernel(const P
   for (int i = 0; i < count; ++i) {
     const int start = start_of(i);
     const uint32_t exists = (uint32_t)__ballot(id >= 0);
-    const float* const v_row = id >= 0 ? static_cast<const float*>(a.V_pages) + offset_of(i, id) : zero_row_f32;
-    auto row_of = [&](int key) { return (uintptr_t)__shfl((unsigned long long)reinterpret_cast<uintptr_t>(v_row), key, kWave); };   // of the tile
     const int id_after = page_of(i + 2);
-    if (some_of(start)) {
-      piece vf[16];
+    if constexpr (NW > 1) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // tile i, requested a tile ago
+      __syncthreads();                                    // of everybody, and the other slot is free
+      if (i + 1 < count) request(i + 1, id_next);
+    }
+    if (active && some_of(start)) {
+      piece vf[16];   // (NW 4: read four at a time, next to the products of the four before)
+      auto read_values = [&](int r) {
+        const float* const v_row = sums + (i & 1) * (TILE / 2) + TILE / 4 + 4 * h * D + E * l32;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) vf[r] = *(const HF_GLOBAL piece*)(row_of(8 * (r >> 2) + 4 * h + (r & 3)) + 4 * E * l32);
-      f32x16 sacc;
+        for (int n = 0; n < 4; ++n) vf[r + n] = *reinterpret_cast<const piece*>(v_row + (2 * r + n) * D);
+      };
+      uint32_t cut = 0;   // a probability of zero does not make a NaN or an infinity vanish: where rows are masked, such values become zero
+      auto cut_values = [&](int r0, int n) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) sacc[r] = 0.0f;
-#pragma unroll
-      for (int c = 0; c < NC; ++c)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sacc = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[c][e], qf[c][e], sacc, 0, 0, 0);
-      if (i + 1 < count) load_keys(kf, i + 1, id_next);
-      if (!all_of(start)) {
-        const uint32_t sees = view.sees_tile(start) & exists, mine = sees >> (4 * h);
-        seen |= sees;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) sacc[r] = masked_score(sacc[r], mine, 8 * (r >> 2) + (r & 3));
-        uint32_t cut = 0;   // a probability of zero does not make a NaN or an infinity vanish: such values become zero here
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
+        for (int r = r0; r < r0 + n; ++r)
 #pragma unroll
           for (int e = 0; e < E; ++e) {
             const uint32_t w = __float_as_uint(vf[r][e]), left = 0x7f800000u - (w & 0x7f800000u);
@@ -131,7 +155,37 @@ __global__ __launch_bounds__(64 * NW * KS, 1) void paged_attn_f32_kernel(const P
             cut |= ~keep;
             vf[r][e] = __uint_as_float(w & keep);
           }
-        odd = odd || __any(cut != 0);
+      };
+      const bool masked = !all_of(start);
+      f32x16 sacc;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sacc[r] = 0.0f;
+      if constexpr (NW > 1) {
+        const float* const k_row = sums + (i & 1) * (TILE / 2) + l32 * D;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const f32x4 k = *reinterpret_cast<const f32x4*>(k_row + 4 * ((2 * c + h) ^ (l32 % UPR)));
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sacc = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e], qf[c][e], sacc, 0, 0, 0);
+        }
+        read_values(0);
+      } else {
+        const float* const v_row = id >= 0 ? static_cast<const float*>(a.V_pages) + offset_of(i, id) : zero_row_f32;
+        auto row_of = [&](int key) { return (uintptr_t)__shfl((unsigned long long)reinterpret_cast<uintptr_t>(v_row), key, kWave); };   // of the tile
+#pragma unroll
+        for (int r = 0; r < 16; ++r) vf[r] = *(const HF_GLOBAL piece*)(row_of(8 * (r >> 2) + 4 * h + (r & 3)) + 4 * E * l32);
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sacc = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[c][e], qf[c][e], sacc, 0, 0, 0);
+        if (i + 1 < count) load_keys(kf, i + 1, id_next);
+      }
+      if (masked) {
+        const uint32_t sees = view.sees_tile(start) & exists, mine = sees >> (4 * h);
+        seen |= sees;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sacc[r] = masked_score(sacc[r], mine, 8 * (r >> 2) + (r & 3));
+        if (NW == 1) cut_values(0, 16);
       } else {
         seen = 1;
       }
@@ -159,10 +213,18 @@ __global__ __launch_bounds__(64 * NW * KS, 1) void paged_attn_f32_kernel(const P
       }
       l_run += psum;
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
+      for (int r = 0; r < 16; r += 4) {
+        if constexpr (NW > 1) {
+          if (masked) cut_values(r, 4);
+          if (r < 12) read_values(r + 4);
+        }
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[r][e], sacc[r], o[e], 0, 0, 0);
-    } else if (i + 1 < count) {
+        for (int n = r; n < r + 4; ++n)
+#pragma unroll
+          for (int e = 0; e < E; ++e) o[e] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[n][e], sacc[n], o[e], 0, 0, 0);
+      }
+      if (masked) odd = odd || __any(cut != 0);
+    } else if (NW == 1 && i + 1 < count) {
       load_keys(kf, i + 1, id_next);
     }
     id = id_next;
@@ -204,6 +266,7 @@ __global__ __launch_bounds__(64 * NW * KS, 1) void paged_attn_f32_kernel(const P
     }
   }
 
+  if (NW > 1) __syncthreads();   // the tiles are done with; the sums take their place
   l_run += __shfl_xor(l_run, 32, kWave);
   if (seen != 0 && m_ref == -INFINITY && l_run == 0.0f) l_run = kOnlyInfinite;
   float* const row = sums + grp * SPAN + (32 * wave + l32) * (D + 4);
@@ -224,6 +287,7 @@ __global__ __launch_bounds__(64 * NW * KS, 1) void paged_attn_f32_kernel(const P
 
 template <int D, int NW, int KS> int launch(const PagedAttnArgs& a, const PagedSchedule& sc, int grid, hipStream_t s) {
   constexpr int kLds = KS * (32 * NW * (D + 4) + 64 * NW) * 4 + 16;
+  static_assert(NW == 1 || 4 * kKeyTile * 4 * D <= kLds, "two slots of two tiles");
   static LdsGrant grant;
   const int rc = grant_lds(grant, reinterpret_cast<const void*>(&paged_attn_f32_kernel<D, NW, KS>), kLds, "hf_paged_attn_fwd");
   if (rc != HF_OK) return rc;
