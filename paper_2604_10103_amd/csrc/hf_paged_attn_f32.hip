@@ -144,17 +144,20 @@ __global__ __launch_bounds__(64 * NW * KS, NW > 1 ? 2 : 1) void paged_attn_f32_k
 #pragma unroll
         for (int n = 0; n < 4; ++n) vf[r + n] = *reinterpret_cast<const piece*>(v_row + (2 * r + n) * D);
       };
-      uint32_t cut = 0;   // a probability of zero does not make a NaN or an infinity vanish: where rows are masked, such values become zero
+      // a probability of zero does not make a NaN or an infinity vanish: where rows are masked, such values become zero
       auto cut_values = [&](int r0, int n) {
+        auto full = [](float v) { return ((__float_as_uint(v) & 0x7f800000u) + 0x00800000u) & 0x80000000u; };   // the top bit: its exponent is full
+        uint32_t any = 0;
 #pragma unroll
         for (int r = r0; r < r0 + n; ++r)
 #pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const uint32_t w = __float_as_uint(vf[r][e]), left = 0x7f800000u - (w & 0x7f800000u);
-            const uint32_t keep = 0u - min(left, 1u);   // all ones where finite
-            cut |= ~keep;
-            vf[r][e] = __uint_as_float(w & keep);
-          }
+          for (int e = 0; e < E; ++e) any |= full(vf[r][e]);
+        if (!__any(any != 0)) return;
+        odd = true;
+#pragma unroll
+        for (int r = r0; r < r0 + n; ++r)
+#pragma unroll
+          for (int e = 0; e < E; ++e) vf[r][e] = __uint_as_float(__float_as_uint(vf[r][e]) & ~(uint32_t)((int)full(vf[r][e]) >> 31));
       };
       const bool masked = !all_of(start);
       f32x16 sacc;
@@ -185,7 +188,7 @@ __global__ __launch_bounds__(64 * NW * KS, NW > 1 ? 2 : 1) void paged_attn_f32_k
         seen |= sees;
 #pragma unroll
         for (int r = 0; r < 16; ++r) sacc[r] = masked_score(sacc[r], mine, 8 * (r >> 2) + (r & 3));
-        if (NW == 1) cut_values(0, 16);
+        if constexpr (NW == 1) cut_values(0, 16);
       } else {
         seen = 1;
       }
@@ -223,7 +226,6 @@ __global__ __launch_bounds__(64 * NW * KS, NW > 1 ? 2 : 1) void paged_attn_f32_k
 #pragma unroll
           for (int e = 0; e < E; ++e) o[e] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[n][e], sacc[n], o[e], 0, 0, 0);
       }
-      if (masked) odd = odd || __any(cut != 0);
     } else if (NW == 1 && i + 1 < count) {
       load_keys(kf, i + 1, id_next);
     }
