@@ -17,13 +17,15 @@ struct PagedAttnArgs {
   const int32_t *cu, *lens, *table;
   float* lse2;
   long long qt, qh, ot, oh;   // strides in elements
-  int n_q, heads, heads_kv, page, n_pages, n_seqs, max_pages, causal, window, n_sink;
+  int n_q, heads, heads_kv, group, page, n_pages, n_seqs, max_pages, causal, window, n_sink;
   float c_scale;              // softmax_scale * log2(e)
   uint32_t page_magic;        // key / page = key * page_magic >> page_shift for key < 2^31
   int page_shift;
-  int page_tiles;             // > 0: key tiles end with their page, of which there are so many in one; tile / page_tiles as above
-  uint32_t tiles_magic;
+  int page_tiles;             // > 0: key tiles end with their page, of which there are so many in one
+  uint32_t tiles_magic;       // as above: tile / page_tiles, row / group (= heads / heads_kv)
   int tiles_shift;
+  uint32_t group_magic;
+  int group_shift;
 };
 size_t paged_workspace_bytes(const hf_paged& c, int n_q);
 int launch_paged_attn(const hf_paged& c, PagedAttnArgs a, void* workspace, hipStream_t s);

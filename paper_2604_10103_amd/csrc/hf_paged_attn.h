@@ -80,6 +80,9 @@ __device__ __forceinline__ int div_page(const PagedAttnArgs& a, int key) {   // 
 __device__ __forceinline__ int div_tiles(const PagedAttnArgs& a, int tile) {
   return (int)(((unsigned long long)(unsigned)tile * a.tiles_magic) >> a.tiles_shift);
 }
+__device__ __forceinline__ int div_group(const PagedAttnArgs& a, int row) {
+  return (int)(((unsigned long long)(unsigned)row * a.group_magic) >> a.group_shift);
+}
 __device__ __forceinline__ int tile_of(const PagedAttnArgs& a, int key) {   // that holds the key
   if (a.page_tiles == 0) return key / kKeyTile;
   const int page = div_page(a, key);
@@ -156,15 +159,14 @@ struct SeqWork {
 template <int BM> __device__ __forceinline__ SeqWork seq_work(const PagedAttnArgs& a, int s) {
   SeqWork q = {0, 0, 0, 0, 1, 1};
   if (s >= a.n_seqs) return q;
-  const int group = a.heads / a.heads_kv;
   q.begin = min(max(a.cu[s], 0), a.n_q);
   q.m = min(max(a.cu[s + 1], q.begin), a.n_q) - q.begin;
   q.len = max(a.lens[s], 0);
   if (q.m > 0) {
-    q.T = (q.m * group + BM - 1) / BM;
+    q.T = (q.m * a.group + BM - 1) / BM;
     const int held = min(q.len, a.max_pages * a.page);
-    q.v0 = max(1, key_tiles(a, q.m, q.len, held, 0, min(q.m, (BM - 1) / group + 1) - 1).n);
-    q.v1 = max(1, key_tiles(a, q.m, q.len, held, (q.T - 1) * BM / group, q.m - 1).n);
+    q.v0 = max(1, key_tiles(a, q.m, q.len, held, 0, min(q.m, div_group(a, BM - 1) + 1) - 1).n);
+    q.v1 = max(1, key_tiles(a, q.m, q.len, held, div_group(a, (q.T - 1) * BM), q.m - 1).n);
   }
   return q;
 }
@@ -174,20 +176,22 @@ struct PagedWork {
   bool shares;
   int C, each, split_each;   // pieces: tiles of a part at most, pieces of a key head, those of them that are parts
   int line, share;           // shares: the line's length for one key head, and a workgroup's share
+  SeqWork first;             // the lane's among the first 64 sequences, and its pieces, so that few of them are looked at once
+  int first_pieces, first_split;
 };
 
 constexpr float kComputeUnits = 256;
 
 // pieces of C tiles: a sequence's parts lie in layers.  Row tile r is in layer p < layers() if it sees more than p C tiles, and so has as many
 // parts as layers that hold it; new tokens see more the later they are, so that layer p holds the row tiles from first_row(p) on
-__device__ __forceinline__ int layers(const SeqWork& q, int C) { return (max(q.v0, q.v1) + C - 1) / C; }
+__device__ __forceinline__ int layers(const SeqWork& q, int C) { return (int)((unsigned)(max(q.v0, q.v1) + C - 1) / (unsigned)C); }
 template <int BM> __device__ __forceinline__ int first_row(const PagedAttnArgs& a, const SeqWork& q, int C, int p) {
   if (!a.causal || p * C < q.v0) return 0;
   const int token = min(max(tile_start(a, p * C) - (q.len - q.m), 0), max(q.m - 1, 0));
-  return min(token * (a.heads / a.heads_kv) / BM, max(q.T - 1, 0));
+  return min(token * a.group / BM, max(q.T - 1, 0));
 }
 template <int BM> __device__ __forceinline__ int pieces_of(const PagedAttnArgs& a, const SeqWork& q, int C) {
-  const int S = layers(q, C), all = a.causal && q.T > 1 ? min(S, (q.v0 + C - 1) / C) : S;
+  const int S = layers(q, C), all = a.causal && q.T > 1 ? min(S, (int)((unsigned)(q.v0 + C - 1) / (unsigned)C)) : S;
   int n = all * q.T;
   for (int p = all; p < S; ++p) n += q.T - first_row<BM>(a, q, C, p);
   return n;
@@ -205,17 +209,17 @@ template <int BM, bool kShares> __device__ __forceinline__ PagedWork find_work(c
   const auto add = [](float x, float y) { return x + y; };
   const auto larger = [](float x, float y) { return fmaxf(x, y); };
   float units = 0.0f, rows = 0.0f, longest = 1.0f;
-  SeqWork q;
+  SeqWork q = {0, 0, 0, 0, 1, 1};
   for (int s0 = 0; s0 < a.n_seqs; s0 += kWave) {
     q = seq_work<BM>(a, s0 + lane);
     // from row tile to row tile what they see grows by their tokens until it is v1 (shrinks, where a window ends and nothing is causal)
     const float v0 = (float)q.v0, v1 = (float)q.v1, T = (float)q.T;
-    const float grows = fminf(T, fabsf(v1 - v0) * (float)(kKeyTile * (a.heads / a.heads_kv)) * (1.0f / BM));
+    const float grows = fminf(T, fabsf(v1 - v0) * (float)(kKeyTile * a.group) * (1.0f / BM));
     units += T * v1 + 0.5f * grows * (v0 - v1);
     rows += T;
     longest = fmaxf(longest, (float)(q.T > 0 ? max(q.v0, q.v1) : 1));
   }
-  PagedWork p = {false, 0x3fffffff, 0, 0, 0, 1};
+  PagedWork p = {false, 0x3fffffff, 0, 0, 0, 1, q, 0, 0};
   if (sc.meets) {
     units = total_of(units, 0.0f, add);
     rows = total_of(rows, 0.0f, add);
@@ -248,26 +252,28 @@ template <int BM, bool kShares> __device__ __forceinline__ PagedWork find_work(c
       if (p.shares) {
         p.line += total_sum(line_at<BM>(q, q.T, sc.lead));
       } else {
-        const int e = pieces_of<BM>(a, q, p.C);
-        p.each += total_sum(e);
-        p.split_each += total_sum(layers(q, p.C) > 1 ? e : 0);
+        p.first_pieces = pieces_of<BM>(a, q, p.C);
+        p.first_split = layers(q, p.C) > 1 ? p.first_pieces : 0;
+        p.each += total_sum(p.first_pieces);
+        p.split_each += total_sum(p.first_split);
       }
     }
     // more than there is room for, which an estimate may come to: nothing is cut
     if (p.shares || !once || (p.split_each * a.heads_kv <= 2 * sc.groups && (kShares || p.each * a.heads_kv <= (int)gridDim.x))) break;
     p.C = 0x3fffffff;
   }
+  p.first = q;
   if (p.shares) p.share = max((int)(((long long)p.line * a.heads_kv + sc.groups - 1) / sc.groups), sc.lead + 3 * kNear);
   return p;
 }
 
 // What both ways have in common: the sequence that holds place y of `extent` a sequence, and what precedes it
-template <int BM, class Extent> __device__ __forceinline__ bool find_seq(const PagedAttnArgs& a, int y, Extent extent, SeqWork& q, int& seq, int& before,
+template <int BM, class Extent> __device__ __forceinline__ bool find_seq(const PagedAttnArgs& a, const PagedWork& p, int y, Extent extent, SeqWork& q, int& seq, int& before,
                                                                         int& split_before) {
   const int lane = thread_id() & 63;
   before = split_before = 0;
   for (int s0 = 0; s0 < a.n_seqs; s0 += kWave) {
-    const SeqWork mine = seq_work<BM>(a, s0 + lane);
+    const SeqWork mine = a.n_seqs > kWave ? seq_work<BM>(a, s0 + lane) : p.first;
     int split = 0;
     const int e = extent(mine, split), upto = scan_sum(e), split_upto = scan_sum(split);
     const unsigned long long owner = __ballot(y >= before + upto - e && y < before + upto);
@@ -287,25 +293,28 @@ template <int BM, class Extent> __device__ __forceinline__ bool find_seq(const P
 }
 
 template <int BM> __device__ __forceinline__ void set_rows(const PagedAttnArgs& a, const SeqWork& q, int seq, int r, PagedItem& it) {
-  const int group = a.heads / a.heads_kv;
   it.seq = seq;
   it.begin = q.begin;
   it.m = q.m;
   it.len = q.len;
   it.held = min(q.len, a.max_pages * a.page);
   it.first = r * BM;
-  it.rows = min(BM, q.m * group - it.first);
-  it.keys = key_tiles(a, q.m, q.len, it.held, it.first / group, (it.first + it.rows - 1) / group);
+  it.rows = min(BM, q.m * a.group - it.first);
+  it.keys = key_tiles(a, q.m, q.len, it.held, div_group(a, it.first), div_group(a, it.first + it.rows - 1));
 }
 
 // pieces: the `item`-th
 template <int BM> __device__ __forceinline__ bool find_piece(const PagedAttnArgs& a, const PagedSchedule& sc, const PagedWork& p, int item, PagedItem& it) {
   if (item >= p.each * a.heads_kv) return false;
-  it.head_kv = item / p.each;
+  it.head_kv = (int)((unsigned)item / (unsigned)p.each);
   const int y = item - it.head_kv * p.each, lane = thread_id() & 63;
   SeqWork q;
   int seq, before, split_before;
-  if (!find_seq<BM>(a, y, [&](const SeqWork& x, int& split) {
+  if (!find_seq<BM>(a, p, y, [&](const SeqWork& x, int& split) {
+        if (a.n_seqs <= kWave) {
+          split = p.first_split;
+          return p.first_pieces;
+        }
         const int e = pieces_of<BM>(a, x, p.C);
         split = layers(x, p.C) > 1 ? e : 0;
         return e;
@@ -314,7 +323,7 @@ template <int BM> __device__ __forceinline__ bool find_piece(const PagedAttnArgs
   const int S = layers(q, p.C), idx = y - before;
   int back, at = 0;   // at: parts of the row tiles behind this one
   if (!a.causal || q.T == 1 || S == 1) {
-    it.part = idx / q.T;
+    it.part = (int)((unsigned)idx / (unsigned)q.T);
     it.parts = S;
     back = idx - it.part * q.T;
     at = back * S;
@@ -356,7 +365,7 @@ template <int BM> __device__ __forceinline__ bool find_part(const PagedAttnArgs&
   const int y = x - it.head_kv * p.line, lane = thread_id() & 63;
   SeqWork q;
   int seq, before, split_before;
-  if (!find_seq<BM>(a, y, [&](const SeqWork& s, int&) { return line_at<BM>(s, s.T, sc.lead); }, q, seq, before, split_before)) return false;
+  if (!find_seq<BM>(a, p, y, [&](const SeqWork& s, int&) { return line_at<BM>(s, s.T, sc.lead); }, q, seq, before, split_before)) return false;
   // the row tile: the last one that starts at or before y
   int lo = 0, span = q.T;
   while (span > 1) {
@@ -475,7 +484,7 @@ template <typename T, int D, int BM, int KS, int NT, class RowsAt, class StatsAt
 __device__ __forceinline__ void finish_item(const PagedAttnArgs& a, const PagedSchedule& sc, const PagedItem& it, RowsAt rows_at, StatsAt stats_at,
                                             int* flag) {
   constexpr int TPR = D / 8, PER = NT / TPR, PASS = (BM + PER - 1) / PER;
-  const int tid = thread_id(), f = 8 * (tid % TPR), r0 = tid / TPR, group = a.heads / a.heads_kv;
+  const int tid = thread_id(), f = 8 * (tid % TPR), r0 = tid / TPR;
   typedef unsigned long long u64;
   __syncthreads();
   auto meet = [&](int row, float* acc, float& M, float& L) {   // the groups' parts of a row
@@ -508,7 +517,7 @@ __device__ __forceinline__ void finish_item(const PagedAttnArgs& a, const PagedS
     if (only && M == -INFINITY && L == 0.0f) L = kOnlyInfinite;
   };
   auto write = [&](int row, const float* acc, float M, float L) {
-    const int x = it.first + row, token = x / group, head = it.head_kv * group + (x - token * group);
+    const int x = it.first + row, token = div_group(a, x), head = it.head_kv * a.group + (x - token * a.group);
     const bool none = M == -INFINITY && L == 0.0f;   // (a NaN anywhere makes L one)
     const float inv = none ? 0.0f : (L == kOnlyInfinite ? __builtin_nanf("") : 1.0f / L);
     float y[8];

@@ -87,15 +87,15 @@ __global__ __launch_bounds__(64 * NW * KS, (NW > 1 ? 2 : 1)) void paged_attn_ker
   const int wave_in_wg = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wave = KS == 1 ? wave_in_wg : 0, grp = KS == 1 ? 0 : wave_in_wg;
   char* const sK = smem + grp * S::SPAN;
-  const int l32 = lane & 31, h = lane >> 5, group = a.heads / a.heads_kv;
+  const int l32 = lane & 31, h = lane >> 5, group = a.group;
 
   // ---- this lane's row (past the item's rows: its last one again; only the rows that there are get stored)
-  const int x_last = it.first + it.rows - 1, x = min(it.first + 32 * wave + l32, x_last), token = x / group;
+  const int x_last = it.first + it.rows - 1, x = min(it.first + 32 * wave + l32, x_last), token = div_group(a, x);
   const RowView view = row_view(a, it, token);
   const bool active = 32 * wave < it.rows;                 // (uniform)
   // what all rows of the wavefront see, and what any of them sees
-  const RowView view_lo = row_view(a, it, min(it.first + 32 * wave, x_last) / group);
-  const RowView view_hi = row_view(a, it, min(it.first + 32 * wave + 31, x_last) / group);
+  const RowView view_lo = row_view(a, it, div_group(a, min(it.first + 32 * wave, x_last)));
+  const RowView view_hi = row_view(a, it, div_group(a, min(it.first + 32 * wave + 31, x_last)));
   bf16x8 qf[NS];
   {
     const bf16_t* q = static_cast<const bf16_t*>(a.Q) + (long long)(it.begin + token) * a.qt +
@@ -244,11 +244,11 @@ __global__ __launch_bounds__(64 * NW * KS, (NW > 1 ? 2 : 1)) void paged_attn_ker
 
   // the rows have to be here before the first request: the compiler does not count requests, and a wait behind them would be one for
   // all of them
+  if constexpr (kBig) find_places(0);
 #pragma unroll
   for (int s = 0; s < NS; ++s) asm volatile("" : "+v"(qf[s]));
   if (count > 0) {
     if constexpr (kBig) {
-      find_places(0);
       v_places = k_places;
       request_big(k_pool, k_places, 0, sK_lds, k_off);
       bytes_next = request_big(v_pool, k_places, 0, sV_lds, v_off);
@@ -542,6 +542,8 @@ size_t paged_workspace_bytes(const hf_paged& c, int n_q) {
 int launch_paged_attn(const hf_paged& c, PagedAttnArgs a, void* workspace, hipStream_t s) {
   const Plan p = plan_of(c, a.n_q);
   a.page_shift = magic_of(c.page_tokens, a.page_magic);
+  a.group = c.heads / c.heads_kv;
+  a.group_shift = magic_of(a.group, a.group_magic);
   PagedSchedule sc = p.sc;
   if (sc.meets) {
     sc.counters = static_cast<unsigned long long*>(workspace);

@@ -47,13 +47,13 @@ __global__ __launch_bounds__(64 * NW * KS, NW > 1 ? 2 : 1) void paged_attn_f32_k
   const int tid = thread_id(), lane = tid & 63;
   const int wave_in_wg = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wave = wave_in_wg % NW, grp = wave_in_wg / NW;
-  const int l32 = lane & 31, h = lane >> 5, group = a.heads / a.heads_kv;
+  const int l32 = lane & 31, h = lane >> 5, group = a.group;
 
-  const int x_last = it.first + it.rows - 1, x = min(it.first + 32 * wave + l32, x_last), token = x / group;
+  const int x_last = it.first + it.rows - 1, x = min(it.first + 32 * wave + l32, x_last), token = div_group(a, x);
   const RowView view = row_view(a, it, token);
   const bool active = 32 * wave < it.rows;
-  const RowView view_lo = row_view(a, it, min(it.first + 32 * wave, x_last) / group);
-  const RowView view_hi = row_view(a, it, min(it.first + 32 * wave + 31, x_last) / group);
+  const RowView view_lo = row_view(a, it, div_group(a, min(it.first + 32 * wave, x_last)));
+  const RowView view_hi = row_view(a, it, div_group(a, min(it.first + 32 * wave + 31, x_last)));
   f32x4 qf[NC];
   {
     const float* q = static_cast<const float*>(a.Q) + (long long)(it.begin + token) * a.qt +
