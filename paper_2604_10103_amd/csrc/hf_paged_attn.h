@@ -351,8 +351,9 @@ template <int BM> __device__ __forceinline__ bool find_piece(const PagedAttnArgs
   it.counter = it.slot0 = it.head_kv * p.split_each + split_before + at;   // (meant where there are parts)
   it.slot1 = it.slot0 + 1;
   it.slot_step = 1;
-  it.t0 = (int)((long long)it.keys.n * it.part / it.parts);
-  it.t1 = (int)((long long)it.keys.n * (it.part + 1) / it.parts);
+  const int each = (int)((unsigned)it.keys.n / (unsigned)it.parts), more = it.keys.n - each * it.parts;   // the first `more` parts have one more
+  it.t0 = each * it.part + min(it.part, more);
+  it.t1 = it.t0 + each + (it.part < more ? 1 : 0);
   return true;
 }
 
