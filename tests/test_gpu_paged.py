@@ -231,6 +231,84 @@ def test_values_that_are_not_finite_reach_their_features(dtype, d, bad, page):
     b.check(torch.tensor(np.where(fine[:, None], got, ref[0]), device=DEV), lse, ref)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new,longest", [([0, 1, 1, 2, 5], 200), ([0, 1, 60, 90], 300)])
+def test_more_sequences_than_a_wavefront_has_lanes(dtype, new, longest):
+    rng = np.random.default_rng(len(new))
+    new = rng.choice(new, size=300)
+    b = Batch(new, new + rng.integers(0, longest, size=300), 4, 2, 64, dtype, 16, rows_behind=2, seed=20)
+    b.check(*b.attend())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,page,count", [(128, 16, 72), (64, 94, 72), (64, 40, 20)])
+def test_long_sequences_of_single_tokens(dtype, d, page, count):
+    """More keys than one round of workgroups takes, of sequences that differ: a workgroup has several sequences, and parts of some."""
+    rng = np.random.default_rng(count)
+    lens = rng.integers(1, 72 * 2500 // count, size=count)
+    lens[3], lens[7] = 0, 1
+    new = rng.choice([1, 1, 1, 3], size=count)
+    b = Batch(new, lens, 8, 4, d, dtype, page, seed=21)
+    ref = b.oracle()
+    O, lse = b.attend()
+    b.check(O, lse, ref)
+    O2, lse2 = b.attend()
+    assert torch.equal(O, O2) and torch.equal(lse, lse2)
+    b = Batch(new, lens, 8, 4, d, dtype, page, seed=22, window=1200, n_sink=50)
+    b.check(*b.attend())
+
+
+@pytest.mark.parametrize("page", [24, 64])
+@pytest.mark.parametrize("mask", [dict(), dict(causal=False, window=700, n_sink=64), dict(window=500)])
+def test_long_chunks_of_many_heads(page, mask):
+    b = Batch([1030, 5, 131], [1300, 400, 131], 32, 32, 128, "bf16", page, seed=23, **mask)
+    b.check(*b.attend())
+
+
+@pytest.mark.parametrize("heads,heads_kv,new,lens", [(4, 1, [900], [900]), (8, 2, [700, 300], [2500, 300]), (2, 2, [1500, 1, 40], [1500, 6000, 3000])])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("window", [0, 600])
+def test_long_causal_chunks_of_few_heads(dtype, heads, heads_kv, new, lens, window):
+    """Few rows for the chip: row tiles have parts, the later ones more of them."""
+    b = Batch(new, lens, heads, heads_kv, 64, dtype, 32, seed=24, window=window, n_sink=window // 50)
+    b.check(*b.attend())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_pools_past_32_bits(dtype):
+    """Pages on both sides of every 4 GiB of the pools, written by the append and read by both shapes of attention."""
+    page, Hk, d = 64, 8, 128
+    size = Hk * page * d * (2 if dtype == "bf16" else 4)
+    n_pages = (9 << 30) // size + 3
+    b = Batch([1, 200, 3], [300, 200, 130], 8, Hk, d, dtype, page, seed=25)
+    used = [int(x) for x in b.table.flatten() if x >= 0]
+    edge = (4 << 30) // size
+    far = [0, edge - 1, edge, edge + 1, 2 * edge - 1, 2 * edge, 2 * edge + 1, n_pages - 1, n_pages - 2, n_pages - 3, 1, 5, 7]
+    assert len(used) <= len(far)
+    K, V = torch.empty((n_pages, Hk, page, d), dtype=b.t, device=DEV), torch.empty((n_pages, Hk, page, d), dtype=b.t, device=DEV)
+    move = dict(zip(used, far))
+    for x, y in move.items():
+        K[y], V[y] = b.K_pages[x], b.V_pages[x]
+    small, cache, table = (b.K_pages, b.V_pages), b.cache, b.table_d
+    want_K, want_V = orc.append(f64(b.K_pages), f64(b.V_pages), f64(b.K), f64(b.V), b.cu, b.lens, b.table)
+    big = hf.make_paged(8, Hk, d, dtype, page, n_pages, 3, b.table.shape[1])
+    far_table = torch.tensor(np.vectorize(lambda x: move.get(x, -1))(b.table), dtype=torch.int32, device=DEV)
+    hf.hf_paged_append(big, b.K, b.V, b.cu_d, b.lens_d, K, V, far_table)
+    for x, y in move.items():
+        assert np.array_equal(f64(K[y]), want_K[x]) and np.array_equal(f64(V[y]), want_V[x])
+    hf.hf_paged_append(cache, b.K, b.V, b.cu_d, b.lens_d, *small, table)
+    ref = b.oracle()
+    O, lse = b.attend()
+    b.check(O, lse, ref)
+    for count in (1, 3):   # the single token alone, and the whole batch
+        n = int(b.cu[count])
+        c = hf.make_paged(8, Hk, d, dtype, page, n_pages, count, b.table.shape[1])
+        ws = torch.empty(max(1, hf.hf_paged_workspace_bytes(c, n)), dtype=torch.uint8, device=DEV)
+        out = torch.empty((n, 8, d), dtype=b.t, device=DEV)
+        hf.hf_paged_attn_fwd(c, b.Q[:n], b.cu_d[:count + 1], b.lens_d[:count], K, V, far_table[:count], out, ws)
+        b.check(torch.cat([out, O[n:]]), None, ref)
+
+
 def test_the_same_bits_every_time_and_in_any_workspace():
     b = Batch([1] * 30 + [70], list(range(1, 6000, 200)) + [900], 8, 2, 128, "bf16", 16, seed=14)
     O, lse = b.attend()
@@ -272,6 +350,67 @@ def test_another_stream():
         O, lse2 = b.attend()
     s.synchronize()
     assert torch.equal(O, want) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_two_captured_calls_share_a_workspace(dtype):
+    """Replays in turn, with eager calls in the same workspace and other lengths in between; every one against an eager call of its own."""
+    a = Batch([1] * 9, [5000, 3, 700, 64, 1, 2500, 33, 900, 4000], 8, 2, 128, dtype, 16, seed=26)
+    b = Batch([150, 3], [6000, 2000], 8, 2, 128, dtype, 64, seed=27)
+    n = max(hf.hf_paged_workspace_bytes(x.cache, x.n) for x in (a, b))
+    ws = torch.randint(0, 255, (n,), dtype=torch.uint8, device=DEV)
+    outs, graphs = [], []
+    full = [x.lens_d.clone() for x in (a, b)]
+    for x in (a, b):
+        x.lens_d.copy_(torch.clamp(x.lens_d, max=40))          # captured with other lengths than replayed
+        O, lse = torch.empty((x.n, 8, 128), dtype=x.t, device=DEV), torch.empty((8, x.n), device=DEV)
+        run = lambda x=x, O=O, lse=lse: hf.hf_paged_attn_fwd(x.cache, x.Q, x.cu_d, x.lens_d, x.K_pages, x.V_pages, x.table_d, O, ws, lse)  # noqa: E731
+        run()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            run()
+        outs.append((O, lse))
+        graphs.append((g, run))
+    for x, n in zip((a, b), full):
+        x.lens_d.copy_(n)
+    want = [x.attend() for x in (a, b)]
+    for x, w in zip((a, b), want):
+        x.check(*w)
+    for k in range(6):
+        for i in (0, 1):
+            outs[i][0].fill_(3.0)
+            graphs[i][0].replay()
+            if k % 2:
+                torch.cuda.synchronize()
+            assert torch.equal(outs[i][0], want[i][0]) and torch.equal(outs[i][1], want[i][1])
+        if k == 2:
+            graphs[0][1]()                                     # eager, in the same workspace
+            assert torch.equal(outs[0][0], want[0][0])
+    a.lens_d.copy_(torch.tensor([1, 2, 5000, 0, 60, 61, 62, 63, 64], dtype=torch.int32))
+    a.lens = a.lens_d.cpu().numpy().astype(np.int64)
+    a.table[2] = a.table[0]                                    # the third sequence is as long as the first was
+    a.table_d.copy_(torch.tensor(a.table, dtype=torch.int32))
+    graphs[0][0].replay()
+    a.check(outs[0][0], None)
+
+
+def test_calls_on_several_streams_at_once():
+    batches = [Batch([1] * 20, list(range(10, 4010, 200)), 8, 2, 128, "bf16", 16, seed=28), Batch([300], [3000], 4, 2, 64, "bf16", 32, seed=29),
+               Batch([2, 1], [9000, 50], 8, 2, 64, "f32", 16, seed=30)]
+    want = [b.attend() for b in batches]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in batches]
+    got = [[] for _ in batches]
+    spaces = [b.workspace() for b in batches]
+    torch.cuda.synchronize()
+    for _ in range(8):
+        for i, (b, s) in enumerate(zip(batches, streams)):
+            with torch.cuda.stream(s):
+                got[i].append(b.attend(workspace=spaces[i]))
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        assert all(torch.equal(O, w[0]) and torch.equal(lse, w[1]) for O, lse in g)
 
 
 def test_no_rows():
