@@ -18,7 +18,7 @@
  *  - `stream` is a hipStream_t passed as void* (NULL = the default stream).  Every call
  *    only enqueues kernels on that stream: no call synchronises, none allocates.
  *  - Tensors are contiguous, head-major [batch, heads, tokens, head_dim] with head_dim
- *    innermost; dtype of Q, K, V, O is cfg->dtype (bf16 or fp32).  The linear state is
+ *    innermost (the calls for a cache of pages: packed rows with strides); dtype of Q, K, V, O is cfg->dtype (bf16 or fp32).  The linear state is
  *    ALWAYS fp32.  Data pointers must be 16-byte aligned.
  *  - Blocks are consecutive runs of block_q / block_kv tokens counted from token 0 of the
  *    buffer; the last block may be short (it is pooled over its real length and only its

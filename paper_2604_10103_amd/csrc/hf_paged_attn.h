@@ -18,8 +18,10 @@
 //           costs; each of `groups` workgroups gets an equal share of the line.  A share's end that falls near a row tile's ends moves
 //           there.  So a workgroup has whole row tiles and at most two parts.
 // Where workgroups of 32 rows have work for more than one round, shares are taken if the model expects them to be faster: 64 single
-// tokens over 500 to 8191 keys 225 us, in pieces 266.  Rows of chunks read the same keys at the same time when they lie in pieces, and
-// find them in the L2; in shares they do not (4680 rows over 9360 keys: 314 us in pieces, 354 in shares).
+// tokens over 500 to 8191 keys 210 us, in pieces 278.  Rows of chunks read the same keys at the same time when they lie in pieces, and
+// find them in the L2; in shares they do not (4680 rows of 12 heads over 9360 keys take an eighth longer).  Nor does it pay to cut off
+// what the longest rows have over the others: 4680 rows that see 10920 to 14040 keys 405 us whole, 429 to 451 with 14 to 22 % cut off.
+// A single token over 4096 keys takes 14.8 us in parts, 34.4 whole; one over 131071 keys (four rows) 114 and 1130.
 //
 // Parts of a row meet in the workspace: each writes its sums (fp32) there, the last one to arrive adds them in the order of the parts.
 #pragma once

@@ -5,14 +5,20 @@
 // so that the statistics of a row are private to its two lanes and the exponentials of S^T are, rounded to bf16, the B operand of the
 // second product.  K and V tiles go global -> LDS directly, V^T fragments are transposing reads, three K slots and two V slots.
 // Here the rows are tokens x heads of a group, and a tile lies in a page.  A wavefront finds out for 64 tiles at once where they lie, a lane
-// each; a tile's descriptor is then a few scalar instructions.  (12 heads x 4680 x 9360: 0.284 ms; with entries of the page table that the
-// scalar unit reads a tile ahead 0.33, they are on their way when the tile's barrier waits for everything that is; with tiles that go on in
-// the next page, and a branch for them, 0.311.)
+// each; a tile's descriptor is then a few scalar instructions.  (12 heads x 4680 x 9360, pages of 1560: 279 us, with an address for every
+// lane instead 322.  Entries of the table that the scalar unit reads a tile ahead cost a sixth: they are on their way when the tile's
+// barrier waits for everything that is; tiles that go on in the next page, and a branch for them, a tenth.)
 //
 // Three shapes of workgroup (NW wavefronts of rows, KS groups of wavefronts that share the keys):
 //   NW 8, KS 1   256 rows, tiles shared by eight wavefronts, one barrier a tile, one workgroup a compute unit (head_dim 128): long chunks
-//   NW 4, KS 1   128 rows, two workgroups a compute unit (head_dim 64: three): chunks.  Both are bound by the matrix cores and the softmax
-//   NW 1, KS 4   32 rows, every wavefront its own tiles and no barrier until the end: single tokens, bound by memory
+//   NW 4, KS 1   128 rows, two workgroups a compute unit (head_dim 64: three): chunks
+//   NW 1, KS 4   32 rows, every wavefront its own tiles and no barrier until the end: single tokens
+// The first two are bound by matrix cores and softmax together, whose instructions a SIMD's two wavefronts issue one after the other, and by
+// power: 12 heads x 4680 x 9360 reach 966 TFLOP/s at the 2.0 GHz that the chip holds there, the matrix cores 44 % of the cycles busy, the
+// vector units 43 %, no LDS conflict.  (Wavefronts that take turns between barriers, one half at the products while the other is at its
+// exponentials, need 360 us for 266: alone, a wavefront leaves a fifth of the vector unit's issue slots empty.)  The last one is bound by
+// memory: 64 single tokens over 500 to 8191 keys in 210 us, 5.6 TB/s; short ones by the chain arguments, lengths, page table, keys
+// (118 keys: 8.4 us, of which 3.3 go until the work is known, 1.5 until the rows are there, 1.4 for a tile, 1.0 for the end).
 #include "hf_paged_attn.h"
 
 namespace hf {
@@ -39,7 +45,9 @@ template <int D> __device__ __forceinline__ int v_swizzle(int r) {
   return D == 128 ? ((r & 3) << 2 | ((r >> 2) & 3)) : (((r >> 1) & 1) << 2 | ((r >> 2) & 3));
 }
 
-// max without the quieting of NaNs around fmaxf: a NaN score makes its row's sum one in any case
+// max without the quieting of NaNs around fmaxf: a NaN score makes its row's sum one in any case.  (Between the products that write the
+// scores and this, which the compiler does not know to read them, lie the reads of the next fragments: more than the 11 issue slots that
+// the results take.)
 __device__ __forceinline__ float max3f(float a, float b, float c) {
   float r;
   asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
@@ -461,7 +469,8 @@ Plan plan_of(const hf_paged& c, int n_q) {
   Plan p = {};
   auto tiles = [&](int of) { return (rows / of + (n_q < c.n_seqs ? n_q : c.n_seqs)) * c.heads_kv; };   // row tiles of all heads, at most
   // A workgroup of 128 rows where a sequence has more than 32 on the average.  256 rows, whose tiles travel half as often, take 0.89 us a
-  // tile where two workgroups of 128 take 1.07, if a compute unit's rounds of them are no more.
+  // tile where two workgroups of 128 take 1.07, if a compute unit's rounds of them are no more (12 heads x 4680 x 9360: 279 and 293 us;
+  // a prompt of 4096, 32 heads on 8: 156 and 161).  The times are fits to launches of 128 to 768 row tiles over 256 to 4096 keys.
   p.rows = rows > 32ll * c.n_seqs ? 128 : 32;
   if (p.rows == 128 && c.dtype == HF_BF16 && c.head_dim == 128 && rows > 128ll * c.n_seqs) {
     const long long n = (rows + c.n_seqs - 1) / c.n_seqs, heads = (long long)c.n_seqs * c.heads_kv;   // (as if all were as long)
@@ -550,7 +559,7 @@ int launch_paged_attn(const hf_paged& c, PagedAttnArgs a, void* workspace, hipSt
     sc.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + align256((size_t)sc.groups * 16));
     sc.tag = next_call_tag();
   }
-  // tiles that end with their page where the last, short ones are a sixteenth at most
+  // tiles that end with their page where the last, short ones are a sixteenth at most (pages of 16 keys would halve every tile)
   const int tiles = (c.page_tokens + kKeyTile - 1) / kKeyTile;
   if (c.dtype == HF_BF16 && tiles * kKeyTile * 16 <= c.page_tokens * 17) {
     a.page_tiles = tiles;

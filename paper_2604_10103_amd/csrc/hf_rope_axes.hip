@@ -1,8 +1,12 @@
 // Rows turned by positions with several axes (hf_rope_axes_apply), and the same on the way into a cache of pages (hf_paged_append).
 //
 // Both move every row once: they are bound by memory.  A thread owns the same few pairs of a token for many heads, so that an angle
-// (a product and a reduction in 64 bits, two polynomials: some fifty instructions) is formed once and serves them all.
+// (a product and a reduction in 64 bits, two polynomials: some fifty instructions) is formed once and serves them all.  10800 tokens of
+// 80 rows turn in 89 us, 5.0 TB/s; two streams' 4680 tokens of 12 keys, values and queries are appended in 42 us, 4.1 TB/s, of which some
+// 4 us are the launch and the chain lengths, page table, rows; a token of 40 rows turns in 4.7 us, 64 single tokens are appended in 5.4.
 #include <math.h>
+
+#include <algorithm>
 
 #include "hf_paged.h"
 #include "hf_rope_axes.h"
@@ -91,11 +95,12 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const AxesSpec spec, 
   }
 }
 
-// shares of a token's rows: enough workgroups to fill the chip
+// shares of a token's rows: 2048 workgroups where that leaves each four rows, which are read together by an angle formed once (9360 tokens of
+// 36 rows: 42 us, with 1024 workgroups 46), else 1024 (5121 tokens of 24 rows in fp32: 16.3 us, with 2048 19.2)
 int shares(long long groups, int rows) {
-  long long s = (2048 + groups - 1) / groups;
-  if (s > rows) s = rows;
-  return s < 1 ? 1 : (int)s;
+  const auto for_groups = [&](int n) { return (n + groups - 1) / groups; };
+  long long s = std::min(for_groups(2048), std::max(for_groups(1024), (long long)rows / 4));
+  return (int)std::max(1ll, std::min(s, (long long)rows));
 }
 
 }  // namespace
