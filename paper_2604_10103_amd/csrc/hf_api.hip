@@ -52,8 +52,13 @@ unsigned long long next_call_tag() {
   static std::atomic<unsigned long long> seq{0};
   unsigned long long cur = seq.load(std::memory_order_relaxed);
   if (cur == 0) {
-    std::random_device rd;
-    unsigned long long start = (((unsigned long long)rd() << 32) ^ rd()) | 1ull;
+    unsigned long long start = reinterpret_cast<uintptr_t>(&cur) * 0x9e3779b97f4a7c15ull;
+    try {
+      std::random_device rd;
+      start = ((unsigned long long)rd() << 32) ^ rd();
+    } catch (...) {   // (no source of random numbers: the stack's place has to do; nothing may be thrown through a C entry)
+    }
+    start |= 1ull;
     seq.compare_exchange_strong(cur, start, std::memory_order_relaxed);   // (one thread's start wins)
   }
   return seq.fetch_add(1, std::memory_order_relaxed) & 0xffffffffffffull;

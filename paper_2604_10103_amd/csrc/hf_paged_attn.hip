@@ -487,7 +487,7 @@ Plan plan_of(const hf_paged& c, int n_q) {
     p.sc.lead = 5;
   } else {
     const bool wide = c.head_dim == 128;
-    p.sc.groups = 131072 / p.rows / 2;
+    p.sc.groups = 65536 / p.rows;   // (at most 512)
     p.sc.meet = 6.0f;
     p.sc.join = 1.0f;
     p.sc.start = 5.0f;
@@ -519,7 +519,8 @@ int magic_of(int d, uint32_t& magic) {
   return 31 + bits;
 }
 
-size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+// The counters' part of every workspace is as large, whatever the call: what a call of another shape left there are counters of its tag
+constexpr size_t kCounterBytes = 2 * 512 * 8;
 
 template <int D, int NW, int KS, bool kBig> int launch(const PagedAttnArgs& a, const PagedSchedule& sc, int grid, hipStream_t s) {
   using S = Shape<D, NW, KS>;
@@ -545,7 +546,7 @@ size_t paged_workspace_bytes(const hf_paged& c, int n_q) {
   if (n_q == 0) return 0;
   const Plan p = plan_of(c, n_q);
   if (!p.sc.meets) return 0;
-  return align256((size_t)p.sc.groups * 16) + (size_t)p.sc.groups * 2 * p.rows * (c.head_dim + 2) * 4;
+  return kCounterBytes + (size_t)p.sc.groups * 2 * p.rows * (c.head_dim + 2) * 4;
 }
 
 int launch_paged_attn(const hf_paged& c, PagedAttnArgs a, void* workspace, hipStream_t s) {
@@ -556,7 +557,7 @@ int launch_paged_attn(const hf_paged& c, PagedAttnArgs a, void* workspace, hipSt
   PagedSchedule sc = p.sc;
   if (sc.meets) {
     sc.counters = static_cast<unsigned long long*>(workspace);
-    sc.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + align256((size_t)sc.groups * 16));
+    sc.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + kCounterBytes);
     sc.tag = next_call_tag();
   }
   // tiles that end with their page where the last, short ones are a sixteenth at most (pages of 16 keys would halve every tile)
