@@ -158,12 +158,17 @@ template <class F> __device__ __forceinline__ float total_of(float v, float neut
 struct SeqWork {
   int begin, m, len, T, v0, v1;
 };
-template <int BM> __device__ __forceinline__ SeqWork seq_work(const PagedAttnArgs& a, int s) {
+struct SeqWords {   // as they lie in memory
+  int begin, end, len;
+};
+__device__ __forceinline__ SeqWords seq_words(const PagedAttnArgs& a, int s) {
+  return s < a.n_seqs ? SeqWords{a.cu[s], a.cu[s + 1], a.lens[s]} : SeqWords{0, 0, 0};
+}
+template <int BM> __device__ __forceinline__ SeqWork seq_work(const PagedAttnArgs& a, const SeqWords& w) {
   SeqWork q = {0, 0, 0, 0, 1, 1};
-  if (s >= a.n_seqs) return q;
-  q.begin = min(max(a.cu[s], 0), a.n_q);
-  q.m = min(max(a.cu[s + 1], q.begin), a.n_q) - q.begin;
-  q.len = max(a.lens[s], 0);
+  q.begin = min(max(w.begin, 0), a.n_q);
+  q.m = min(max(w.end, q.begin), a.n_q) - q.begin;
+  q.len = max(w.len, 0);
   if (q.m > 0) {
     q.T = (q.m * a.group + BM - 1) / BM;
     const int held = min(q.len, a.max_pages * a.page);
@@ -172,14 +177,30 @@ template <int BM> __device__ __forceinline__ SeqWork seq_work(const PagedAttnArg
   }
   return q;
 }
+// f(the lane's sequence) for every 64 sequences, the next ones on their way meanwhile
+template <int BM, class F> __device__ __forceinline__ void each_64(const PagedAttnArgs& a, F f) {
+  const int lane = thread_id() & 63;
+  SeqWords next = seq_words(a, lane);
+#pragma unroll 1
+  for (int s0 = 0; s0 < a.n_seqs; s0 += kWave) {
+    const SeqWords now = next;
+    if (s0 + kWave < a.n_seqs) next = seq_words(a, s0 + kWave + lane);
+    f(seq_work<BM>(a, now));
+  }
+}
 
 // how the work is shared out (uniform)
 struct PagedWork {
   bool shares;
   int C, each, split_each;   // pieces: tiles of a part at most, pieces of a key head, those of them that are parts
   int line, share;           // shares: the line's length for one key head, and a workgroup's share
-  SeqWork first;             // the lane's among the first 64 sequences, and its pieces, so that few of them are looked at once
-  int first_pieces, first_split;
+};
+
+// 64 sequences that are looked at: the lane's, what it extends over, how many of its pieces are parts, and what the sequences before extend over
+struct SeqBlock {
+  int s0;   // the first of them; < 0: none yet
+  SeqWork q;
+  int extent, split, before, split_before;
 };
 
 constexpr float kComputeUnits = 256;
@@ -206,22 +227,28 @@ template <int BM> __device__ __forceinline__ int line_at(const SeqWork& q, int r
   return (int)floor((double)r * (double)(q.v0 + lead) + slope * (double)r * (double)(r - 1));
 }
 
-template <int BM, bool kShares> __device__ __forceinline__ PagedWork find_work(const PagedAttnArgs& a, const PagedSchedule& sc) {
+template <int BM> __device__ __forceinline__ void find_extent(const PagedAttnArgs& a, const PagedSchedule& sc, const PagedWork& p, SeqBlock& block) {
+  block.extent = p.shares ? line_at<BM>(block.q, block.q.T, sc.lead) : pieces_of<BM>(a, block.q, p.C);
+  block.split = !p.shares && layers(block.q, p.C) > 1 ? block.extent : 0;
+}
+
+template <int BM, bool kShares> __device__ __forceinline__ PagedWork find_work(const PagedAttnArgs& a, const PagedSchedule& sc, SeqBlock& block) {
   const int lane = thread_id() & 63;
   const auto add = [](float x, float y) { return x + y; };
   const auto larger = [](float x, float y) { return fmaxf(x, y); };
   float units = 0.0f, rows = 0.0f, longest = 1.0f;
   SeqWork q = {0, 0, 0, 0, 1, 1};
-  for (int s0 = 0; s0 < a.n_seqs; s0 += kWave) {
-    q = seq_work<BM>(a, s0 + lane);
+  each_64<BM>(a, [&](const SeqWork& of) {
+    q = of;
     // from row tile to row tile what they see grows by their tokens until it is v1 (shrinks, where a window ends and nothing is causal)
     const float v0 = (float)q.v0, v1 = (float)q.v1, T = (float)q.T;
     const float grows = fminf(T, fabsf(v1 - v0) * (float)(kKeyTile * a.group) * (1.0f / BM));
     units += T * v1 + 0.5f * grows * (v0 - v1);
     rows += T;
     longest = fmaxf(longest, (float)(q.T > 0 ? max(q.v0, q.v1) : 1));
-  }
-  PagedWork p = {false, 0x3fffffff, 0, 0, 0, 1, q, 0, 0};
+  });
+  PagedWork p = {false, 0x3fffffff, 0, 0, 0, 1};
+  block = SeqBlock{-1, q, 0, 0, 0, 0};
   if (sc.meets) {
     units = total_of(units, 0.0f, add);
     rows = total_of(rows, 0.0f, add);
@@ -249,49 +276,56 @@ template <int BM, bool kShares> __device__ __forceinline__ PagedWork find_work(c
   p.shares = kShares && __builtin_amdgcn_readfirstlane((int)p.shares);
   for (bool once = true;; once = false) {
     p.each = p.split_each = p.line = 0;
-    for (int s0 = 0; s0 < a.n_seqs; s0 += kWave) {
-      if (a.n_seqs > kWave) q = seq_work<BM>(a, s0 + lane);
-      if (p.shares) {
-        p.line += total_sum(line_at<BM>(q, q.T, sc.lead));
-      } else {
-        p.first_pieces = pieces_of<BM>(a, q, p.C);
-        p.first_split = layers(q, p.C) > 1 ? p.first_pieces : 0;
-        p.each += total_sum(p.first_pieces);
-        p.split_each += total_sum(p.first_split);
-      }
-    }
+    const auto count = [&](const SeqWork& of) {
+      block.q = of;
+      find_extent<BM>(a, sc, p, block);
+      const int sum = total_sum(block.extent);
+      p.line += p.shares ? sum : 0;
+      p.each += p.shares ? 0 : sum;
+      p.split_each += total_sum(block.split);
+    };
+    if (a.n_seqs > kWave) each_64<BM>(a, count);
+    else count(q);   // (they stay)
     // more than there is room for, which an estimate may come to: nothing is cut
     if (p.shares || !once || (p.split_each * a.heads_kv <= 2 * sc.groups && (kShares || p.each * a.heads_kv <= (int)gridDim.x))) break;
     p.C = 0x3fffffff;
   }
-  p.first = q;
+  if (a.n_seqs <= kWave) block.s0 = 0;
   if (p.shares) p.share = max((int)(((long long)p.line * a.heads_kv + sc.groups - 1) / sc.groups), sc.lead + 3 * kNear);
   return p;
 }
 
-// What both ways have in common: the sequence that holds place y of `extent` a sequence, and what precedes it
-template <int BM, class Extent> __device__ __forceinline__ bool find_seq(const PagedAttnArgs& a, const PagedWork& p, int y, Extent extent, SeqWork& q, int& seq, int& before,
-                                                                        int& split_before) {
+// What both ways have in common: the sequence that holds place y, and what precedes it.  The 64 sequences that are looked at stay: a workgroup's
+// next item is among them or behind, but for another head's (512 single tokens over 13 to 250 keys 199 us when every item began at the first)
+template <int BM> __device__ __forceinline__ bool find_seq(const PagedAttnArgs& a, const PagedSchedule& sc, const PagedWork& p, int y, SeqBlock& block,
+                                                          SeqWork& q, int& seq, int& before, int& split_before) {
   const int lane = thread_id() & 63;
-  before = split_before = 0;
-  for (int s0 = 0; s0 < a.n_seqs; s0 += kWave) {
-    const SeqWork mine = a.n_seqs > kWave ? seq_work<BM>(a, s0 + lane) : p.first;
-    int split = 0;
-    const int e = extent(mine, split), upto = scan_sum(e), split_upto = scan_sum(split);
-    const unsigned long long owner = __ballot(y >= before + upto - e && y < before + upto);
+  if (block.s0 < 0 || y < block.before) {
+    if (block.s0 != 0) {
+      block.q = seq_work<BM>(a, seq_words(a, lane));
+      find_extent<BM>(a, sc, p, block);
+    }
+    block.s0 = block.before = block.split_before = 0;
+  }
+  while (true) {
+    const int upto = block.before + scan_sum(block.extent), split_upto = block.split_before + scan_sum(block.split);
+    const unsigned long long owner = __ballot(y >= upto - block.extent && y < upto);
     if (owner) {
       const int src = __ffsll(owner) - 1;
       auto of = [&](int v) { return __builtin_amdgcn_readlane(v, src); };
-      q = SeqWork{of(mine.begin), of(mine.m), of(mine.len), of(mine.T), of(mine.v0), of(mine.v1)};
-      seq = s0 + src;
-      before += of(upto - e);
-      split_before += of(split_upto - split);
+      q = SeqWork{of(block.q.begin), of(block.q.m), of(block.q.len), of(block.q.T), of(block.q.v0), of(block.q.v1)};
+      seq = block.s0 + src;
+      before = of(upto - block.extent);
+      split_before = of(split_upto - block.split);
       return true;
     }
-    before += __builtin_amdgcn_readlane(upto, 63);
-    split_before += __builtin_amdgcn_readlane(split_upto, 63);
+    if (block.s0 + kWave >= a.n_seqs) return false;
+    block.s0 += kWave;
+    block.before = __builtin_amdgcn_readlane(upto, 63);
+    block.split_before = __builtin_amdgcn_readlane(split_upto, 63);
+    block.q = seq_work<BM>(a, seq_words(a, block.s0 + lane));
+    find_extent<BM>(a, sc, p, block);
   }
-  return false;
 }
 
 template <int BM> __device__ __forceinline__ void set_rows(const PagedAttnArgs& a, const SeqWork& q, int seq, int r, PagedItem& it) {
@@ -306,21 +340,14 @@ template <int BM> __device__ __forceinline__ void set_rows(const PagedAttnArgs& 
 }
 
 // pieces: the `item`-th
-template <int BM> __device__ __forceinline__ bool find_piece(const PagedAttnArgs& a, const PagedSchedule& sc, const PagedWork& p, int item, PagedItem& it) {
+template <int BM> __device__ __forceinline__ bool find_piece(const PagedAttnArgs& a, const PagedSchedule& sc, const PagedWork& p, int item, SeqBlock& block,
+                                                           PagedItem& it) {
   if (item >= p.each * a.heads_kv) return false;
   it.head_kv = (int)((unsigned)item / (unsigned)p.each);
   const int y = item - it.head_kv * p.each, lane = thread_id() & 63;
   SeqWork q;
   int seq, before, split_before;
-  if (!find_seq<BM>(a, p, y, [&](const SeqWork& x, int& split) {
-        if (a.n_seqs <= kWave) {
-          split = p.first_split;
-          return p.first_pieces;
-        }
-        const int e = pieces_of<BM>(a, x, p.C);
-        split = layers(x, p.C) > 1 ? e : 0;
-        return e;
-      }, q, seq, before, split_before)) return false;
+  if (!find_seq<BM>(a, sc, p, y, block, q, seq, before, split_before)) return false;
   // within a sequence: layer, then rows, the last ones (which see most) first.  A row tile's parts have consecutive places in the workspace
   const int S = layers(q, p.C), idx = y - before;
   int back, at = 0;   // at: parts of the row tiles behind this one
@@ -361,14 +388,14 @@ template <int BM> __device__ __forceinline__ bool find_piece(const PagedAttnArgs
 
 // shares: the part at place x of the line, if it is workgroup `wg`'s (parts of a row tile belong to consecutive ones); else, parts = 0.
 // next: where the row tile ends
-template <int BM> __device__ __forceinline__ bool find_part(const PagedAttnArgs& a, const PagedSchedule& sc, const PagedWork& p, int wg, int x, PagedItem& it,
+template <int BM> __device__ __forceinline__ bool find_part(const PagedAttnArgs& a, const PagedSchedule& sc, const PagedWork& p, int wg, int x, SeqBlock& block, PagedItem& it,
                                                            int& next) {
   it.head_kv = x / p.line;
   if (it.head_kv >= a.heads_kv) return false;
   const int y = x - it.head_kv * p.line, lane = thread_id() & 63;
   SeqWork q;
   int seq, before, split_before;
-  if (!find_seq<BM>(a, p, y, [&](const SeqWork& s, int&) { return line_at<BM>(s, s.T, sc.lead); }, q, seq, before, split_before)) return false;
+  if (!find_seq<BM>(a, sc, p, y, block, q, seq, before, split_before)) return false;
   // the row tile: the last one that starts at or before y
   int lo = 0, span = q.T;
   while (span > 1) {
@@ -406,11 +433,12 @@ template <int BM> __device__ __forceinline__ bool find_part(const PagedAttnArgs&
 // and may have shares; else workgroup ids go round the XCDs so that each takes one contiguous eighth of the pieces, which read the same keys
 struct PagedCursor {
   PagedWork work;
+  SeqBlock block;
   int at, end;
 };
 template <int BM, bool kStay> __device__ __forceinline__ PagedCursor first_item(const PagedAttnArgs& a, const PagedSchedule& sc) {
   PagedCursor c;
-  c.work = find_work<BM, kStay>(a, sc);
+  c.work = find_work<BM, kStay>(a, sc, c.block);
   const int id = (int)blockIdx.x;
   if (!kStay) {   // (the grid is a multiple of eight, and has at least as many workgroups as there are pieces)
     const int per = (c.work.each * a.heads_kv + 7) / 8;
@@ -427,13 +455,13 @@ template <int BM, bool kStay> __device__ __forceinline__ PagedCursor first_item(
 }
 template <int BM, bool kStay> __device__ __forceinline__ bool next_item(const PagedAttnArgs& a, const PagedSchedule& sc, PagedCursor& c, PagedItem& it) {
   if (!kStay || !c.work.shares) {
-    if (c.at >= c.end || !find_piece<BM>(a, sc, c.work, c.at, it)) return false;
+    if (c.at >= c.end || !find_piece<BM>(a, sc, c.work, c.at, c.block, it)) return false;
     c.at += (int)gridDim.x;
     return true;
   }
   while (c.at < c.end) {
     int next;
-    if (!find_part<BM>(a, sc, c.work, blockIdx.x, c.at, it, next)) return false;
+    if (!find_part<BM>(a, sc, c.work, blockIdx.x, c.at, c.block, it, next)) return false;
     const bool mine = it.parts > 0;
     c.at = mine && it.part < it.parts - 1 ? c.end : next;   // (a cut is the share's end)
     if (mine) return true;
