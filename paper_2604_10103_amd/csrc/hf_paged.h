@@ -30,6 +30,6 @@ struct PagedAttnArgs {
 size_t paged_workspace_bytes(const hf_paged& c, int n_q);
 int launch_paged_attn(const hf_paged& c, PagedAttnArgs a, void* workspace, hipStream_t s);
 struct PagedSchedule;
-int launch_paged_attn_f32(const hf_paged& c, const PagedAttnArgs& a, const PagedSchedule& sc, int rows, int grid, hipStream_t s);
+int launch_paged_attn_f32(const hf_paged& c, const PagedAttnArgs& a, const PagedSchedule& sc, int rows, int ks, int grid, hipStream_t s);
 
 }  // namespace hf

@@ -8,11 +8,11 @@
 //
 //   pieces  A row tile that sees w tiles is cut into ceil(w / C) parts of equal length, C = ceil(longest w / S); a workgroup takes a (key
 //           head, sequence, part, rows).  S is the best of 64 candidates, one a lane, by a model of the launch: with n = the
-//           work in row tiles as long as the longest and x = n S / compute units,
+//           work in row tiles as long as the longest and x = n S / units,
 //               rounds(x) (longest w / S * t(x) + start) + (S > 1 ? meet + join S : 0)  microseconds,
-//           rounds(x) = x rounded up where all pieces are as long, else x + 1/2 (single tokens: 3/4), and t(x) what a tile takes: `tile` where
-//           the compute units are full, and next to an idle half of them more (chunks) or, bound by memory, less (single tokens) than its share.  Only S with
-//           n S <= groups are looked at, and S = 1.
+//           rounds(x) = x rounded up where all pieces are as long, else x + 1/2 (single tokens: 3/4), and t(x) what a tile takes: `tile`
+//           where the units are full, and next to an idle half of them more (chunks) or, bound by memory, less (single tokens) than its
+//           share.  Only S with n S <= groups are looked at, and S = 1.
 //   shares  (few rows, where no two workgroups read the same keys) All row tiles of all key heads lie on one line, each as long as its
 //           key tiles (between a sequence's first and last row tile they are taken to grow evenly) and `lead` more for what its start
 //           costs; each of `groups` workgroups gets an equal share of the line.  A share's end that falls near a row tile's ends moves
@@ -40,6 +40,7 @@ struct PagedSchedule {
   bool meets;                    // there is a workspace: 2 groups parts, and as many counters
   float tile, tile_alone;        // microseconds a tile takes where the chip is full, and alone on a compute unit
   float start, meet, join;
+  float units;                   // workgroups that work at a time: the compute units, or four a unit
   unsigned long long* counters;  // [2 groups] arrivals at a row tile
   float* parts;                  // [2 groups][BM][D], behind them [2 groups][BM][2]: row maximum and sum
   unsigned long long tag;
@@ -203,7 +204,6 @@ struct SeqBlock {
   int extent, split, before, split_before;
 };
 
-constexpr float kComputeUnits = 256;
 
 // pieces of C tiles: a sequence's parts lie in layers.  Row tile r is in layer p < layers() if it sees more than p C tiles, and so has as many
 // parts as layers that hold it; new tokens see more the later they are, so that layer p holds the row tiles from first_row(p) on
@@ -255,9 +255,10 @@ template <int BM, bool kShares> __device__ __forceinline__ PagedWork find_work(c
     longest = total_of(longest, 0.0f, larger);
     const float heads = (float)a.heads_kv, n = units / longest * heads;
     const float S = lane < 32 ? (float)(lane + 1) : floorf(32.0f * __builtin_amdgcn_exp2f((float)(lane - 31) * (5.0f / 32.0f)));   // .. 1024
-    const float x = n * S * (1.0f / kComputeUnits), full = fminf(x, 1.0f);
+    const float x = n * S * (1.0f / sc.units), full = fminf(x, 1.0f);
     const bool alike = units > 0.98f * longest * rows || (!kShares && lane > 0);
-    const float rounds = x <= 1.0f ? 1.0f : (alike ? ceilf(x) : x + (kShares ? 0.75f : 0.5f));
+    const bool once = kShares ? x <= 1.0f && rows * heads <= sc.units : x <= 1.0f;   // (those that stay have theirs from the beginning)
+    const float rounds = once ? 1.0f : (alike ? ceilf(x) : x + (kShares ? 0.75f : 0.5f));
     const float work = kShares ? rounds * fmaxf(sc.tile_alone + 0.3f * sc.tile * full, sc.tile * full)
                                : rounds * sc.tile + (rounds - 2.0f * floorf(0.5f * rounds)) * (sc.tile_alone - sc.tile);
     float cost = longest / S * work + rounds * sc.start + (lane > 0 ? sc.meet + sc.join * S : 0.0f);
@@ -267,7 +268,7 @@ template <int BM, bool kShares> __device__ __forceinline__ PagedWork find_work(c
     const float s_best = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(S), at));
     if constexpr (kShares) {
     const float line = (units + rows * (float)sc.lead) * heads;
-    const float by_shares = line * (1.0f / kComputeUnits) * sc.tile + 2.0f * sc.start + sc.meet + 3.0f * sc.join;
+    const float by_shares = line * (1.0f / sc.units) * sc.tile + 2.0f * sc.start + sc.meet + 3.0f * sc.join;
     p.shares = line < 1e9f && line > (float)(sc.groups * (sc.lead + 3 * kNear)) && by_shares < best;
     }
     if (!p.shares && at > 0) p.C = (int)ceilf(longest / s_best);
@@ -296,7 +297,7 @@ template <int BM, bool kShares> __device__ __forceinline__ PagedWork find_work(c
 }
 
 // What both ways have in common: the sequence that holds place y, and what precedes it.  The 64 sequences that are looked at stay: a workgroup's
-// next item is among them or behind, but for another head's (512 single tokens over 13 to 250 keys 199 us when every item began at the first)
+// next item is among them or behind, but for another head's (2048 single tokens over 3 to 60 keys 1096 us when every item began at the first, then 618)
 template <int BM> __device__ __forceinline__ bool find_seq(const PagedAttnArgs& a, const PagedSchedule& sc, const PagedWork& p, int y, SeqBlock& block,
                                                           SeqWork& q, int& seq, int& before, int& split_before) {
   const int lane = thread_id() & 63;

@@ -9,14 +9,15 @@
 // lane instead 322.  Entries of the table that the scalar unit reads a tile ahead cost a sixth: they are on their way when the tile's
 // barrier waits for everything that is; tiles that go on in the next page, and a branch for them, a tenth.)
 //
-// Three shapes of workgroup (NW wavefronts of rows, KS groups of wavefronts that share the keys):
+// Four shapes of workgroup (NW wavefronts of rows, KS groups of wavefronts that share the keys):
 //   NW 8, KS 1   256 rows, tiles shared by eight wavefronts, one barrier a tile, one workgroup a compute unit (head_dim 128): long chunks
 //   NW 4, KS 1   128 rows, two workgroups a compute unit (head_dim 64: three): chunks
 //   NW 1, KS 4   32 rows, every wavefront its own tiles and no barrier until the end: single tokens
+//   NW 1, KS 1   the same by one wavefront, four workgroups a compute unit: single tokens of many sequences
 // The first two are bound by matrix cores and softmax together, whose instructions a SIMD's two wavefronts issue one after the other, and by
 // power: 12 heads x 4680 x 9360 reach 966 TFLOP/s at the 2.0 GHz that the chip holds there, the matrix cores 44 % of the cycles busy, the
 // vector units 43 %, no LDS conflict.  (Wavefronts that take turns between barriers, one half at the products while the other is at its
-// exponentials, need 360 us for 266: alone, a wavefront leaves a fifth of the vector unit's issue slots empty.)  The last one is bound by
+// exponentials, need 360 us for 266: alone, a wavefront leaves a fifth of the vector unit's issue slots empty.)  The others are bound by
 // memory: 64 single tokens over 500 to 8191 keys in 210 us, 5.6 TB/s; short ones by the chain arguments, lengths, page table, keys
 // (118 keys: 8.4 us, of which 3.3 go until the work is known, 1.5 until the rows are there, 1.4 for a tile, 1.0 for the end).
 #include "hf_paged_attn.h"
@@ -459,7 +460,7 @@ __global__ __launch_bounds__(64 * NW * KS, (NW > 1 ? 2 : 1)) void paged_attn_ker
 
 // ---- launches
 struct Plan {
-  int rows, grid;   // rows of a workgroup
+  int rows, grid, ks;   // rows of a workgroup, groups that share their keys
   PagedSchedule sc;
 };
 
@@ -477,7 +478,23 @@ Plan plan_of(const hf_paged& c, int n_q) {
     auto rounds = [&](int of) { return (double)(((n + of - 1) / of * heads + 255) / 256); };
     if (rounds(256) * 0.89 <= rounds(128) * 0.535) p.rows = 256;
   }
-  if (p.rows == 32) {
+  p.ks = p.rows == 32 ? 4 : 1;
+  p.sc.units = 256.0f;
+  // A row tile a wavefront where there are enough for all: its chain (rows, page table, first keys) then passes next to three others'.  512
+  // sequences of 13 to 250 keys, 8 key heads: 98 us, with four wavefronts a row tile 192; 256 of 150 to 3000: 308 and 305; 128 of 400 to
+  // 8000: 397 and 378
+  if (p.rows == 32 && tiles(32) >= 1024) {
+    p.ks = 1;
+    p.sc.groups = 1024;
+    p.sc.units = 1024.0f;
+    const float bytes = (c.head_dim == 128 ? 1.0f : 0.5f) * (c.dtype == HF_F32 ? 2.0f : 1.0f);
+    p.sc.tile = 2.8f * bytes;
+    p.sc.tile_alone = 1.9f * bytes;
+    p.sc.start = 4.0f;
+    p.sc.meet = 5.0f;
+    p.sc.join = 0.1f;
+    p.sc.lead = 2;
+  } else if (p.rows == 32) {
     p.sc.groups = 256;
     p.sc.tile = 0.8f;
     p.sc.tile_alone = 0.27f;
@@ -520,7 +537,7 @@ int magic_of(int d, uint32_t& magic) {
 }
 
 // The counters' part of every workspace is as large, whatever the call: what a call of another shape left there are counters of its tag
-constexpr size_t kCounterBytes = 2 * 512 * 8;
+constexpr size_t kCounterBytes = 2 * 1024 * 8;
 
 template <int D, int NW, int KS, bool kBig> int launch(const PagedAttnArgs& a, const PagedSchedule& sc, int grid, hipStream_t s) {
   using S = Shape<D, NW, KS>;
@@ -537,6 +554,7 @@ template <int D> int launch_of(const PagedAttnArgs& a, const PagedSchedule& sc, 
     if (p.rows == 256) return big ? launch<D, 8, 1, true>(a, sc, p.grid, s) : launch<D, 8, 1, false>(a, sc, p.grid, s);
   }
   if (p.rows == 128) return big ? launch<D, 4, 1, true>(a, sc, p.grid, s) : launch<D, 4, 1, false>(a, sc, p.grid, s);
+  if (p.ks == 1) return big ? launch<D, 1, 1, true>(a, sc, p.grid, s) : launch<D, 1, 1, false>(a, sc, p.grid, s);
   return big ? launch<D, 1, 4, true>(a, sc, p.grid, s) : launch<D, 1, 4, false>(a, sc, p.grid, s);
 }
 
@@ -566,7 +584,7 @@ int launch_paged_attn(const hf_paged& c, PagedAttnArgs a, void* workspace, hipSt
     a.page_tiles = tiles;
     a.tiles_shift = magic_of(tiles, a.tiles_magic);
   }
-  if (c.dtype == HF_F32) return launch_paged_attn_f32(c, a, sc, p.rows, p.grid, s);
+  if (c.dtype == HF_F32) return launch_paged_attn_f32(c, a, sc, p.rows, p.ks, p.grid, s);
   return c.head_dim == 128 ? launch_of<128>(a, sc, p, s) : launch_of<64>(a, sc, p, s);
 }
 

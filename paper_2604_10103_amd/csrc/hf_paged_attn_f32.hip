@@ -10,6 +10,7 @@
 //                (With tiles that every wavefront reads for itself a prompt of 2048 tokens, 8 heads, took 152 us, now 120)
 //   NW 1, KS 4   32 rows, bound by memory: every wavefront reads its own tiles from memory to registers.  32 sequences of 4096 tokens,
 //                8 heads: 220 us, 4.9 TB/s
+//   NW 1, KS 1   the same, a row tile a wavefront, for many sequences (300 of 25 to 500 tokens: 178 us, by four wavefronts each 258)
 #include "hf_paged_attn.h"
 
 namespace hf {
@@ -302,9 +303,10 @@ template <int D, int NW, int KS> int launch(const PagedAttnArgs& a, const PagedS
 
 }  // namespace
 
-int launch_paged_attn_f32(const hf_paged& c, const PagedAttnArgs& a, const PagedSchedule& sc, int rows, int grid, hipStream_t s) {
-  if (c.head_dim == 128) return rows == 128 ? launch<128, 4, 1>(a, sc, grid, s) : launch<128, 1, 4>(a, sc, grid, s);
-  return rows == 128 ? launch<64, 4, 1>(a, sc, grid, s) : launch<64, 1, 4>(a, sc, grid, s);
+int launch_paged_attn_f32(const hf_paged& c, const PagedAttnArgs& a, const PagedSchedule& sc, int rows, int ks, int grid, hipStream_t s) {
+  if (rows == 128) return c.head_dim == 128 ? launch<128, 4, 1>(a, sc, grid, s) : launch<64, 4, 1>(a, sc, grid, s);
+  if (ks == 1) return c.head_dim == 128 ? launch<128, 1, 1>(a, sc, grid, s) : launch<64, 1, 1>(a, sc, grid, s);
+  return c.head_dim == 128 ? launch<128, 1, 4>(a, sc, grid, s) : launch<64, 1, 4>(a, sc, grid, s);
 }
 
 }  // namespace hf

@@ -233,15 +233,16 @@ def test_values_that_are_not_finite_reach_their_features(dtype, d, bad, page):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("new,longest", [([0, 1, 1, 2, 5], 200), ([0, 1, 60, 90], 300)])
-def test_more_sequences_than_a_wavefront_has_lanes(dtype, new, longest):
+@pytest.mark.parametrize("heads,heads_kv,d", [(4, 2, 64), (8, 4, 64), (4, 4, 128)])
+def test_more_sequences_than_a_wavefront_has_lanes(dtype, new, longest, heads, heads_kv, d):
     rng = np.random.default_rng(len(new))
     new = rng.choice(new, size=300)
-    b = Batch(new, new + rng.integers(0, longest, size=300), 4, 2, 64, dtype, 16, rows_behind=2, seed=20)
+    b = Batch(new, new + rng.integers(0, longest, size=300), heads, heads_kv, d, dtype, 16, rows_behind=2, seed=20)
     b.check(*b.attend())
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("d,page,count", [(128, 16, 72), (64, 94, 72), (64, 40, 20)])
+@pytest.mark.parametrize("d,page,count", [(128, 16, 72), (64, 94, 72), (64, 40, 20), (128, 16, 300), (64, 94, 300)])
 def test_long_sequences_of_single_tokens(dtype, d, page, count):
     """More keys than one round of workgroups takes, of sequences that differ: a workgroup has several sequences, and parts of some."""
     rng = np.random.default_rng(count)
