@@ -409,7 +409,8 @@ template <int BM> __device__ __forceinline__ bool find_part(const PagedAttnArgs&
   const int to = x - y + before + __builtin_amdgcn_readfirstlane(line_at<BM>(q, lo + 1, sc.lead));
   next = to;
   // the shares' ends g share that cut it: g = g0 .. g1
-  const int g0 = (from + sc.lead + kNear + p.share - 1) / p.share, g1 = (to - kNear) / p.share, cuts = max(0, g1 - g0 + 1);
+  // (one near its beginning, but before its end: the whole row tile is the next workgroup's, which begins inside it)
+  const int g0 = (min(from + sc.lead + kNear, to) + p.share - 1) / p.share, g1 = (to - kNear) / p.share, cuts = max(0, g1 - g0 + 1);
   it.part = min(max(x / p.share - g0 + 1, 0), cuts);
   it.parts = cuts + 1;
   if (g0 - 1 + it.part != wg) {

@@ -259,6 +259,17 @@ def test_long_sequences_of_single_tokens(dtype, d, page, count):
     b.check(*b.attend())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("short,count,heads", [(96, 110, 8), (64, 118, 8), (32, 100, 8), (20, 300, 4), (96, 300, 4)])
+def test_short_sequences_end_where_a_share_does(dtype, d, short, count, heads):
+    """Short sequences between long ones: workgroups' shares of the work end at, before and behind the ends of the short ones."""
+    lens = np.full(count, short)
+    lens[::2] = 1024
+    b = Batch([1] * count, lens, heads, heads, d, dtype, 16, seed=31)
+    b.check(*b.attend())
+
+
 @pytest.mark.parametrize("page", [24, 64])
 @pytest.mark.parametrize("mask", [dict(), dict(causal=False, window=700, n_sink=64), dict(window=500)])
 def test_long_chunks_of_many_heads(page, mask):
