@@ -270,6 +270,18 @@ def test_short_sequences_end_where_a_share_does(dtype, d, short, count, heads):
     b.check(*b.attend())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("mask", [dict(), dict(causal=False), dict(window=900, n_sink=40), dict(causal=False, window=900, n_sink=40)])
+@pytest.mark.parametrize("count,new,page", [(100, [0, 0, 0, 1, 3, 260], 16), (70, [0, 0, 1, 40, 700], 64), (90, [0, 1, 1, 2], 64)])
+def test_parts_of_many_sequences(dtype, mask, count, new, page):
+    """More sequences than a wavefront has lanes, few rows, long contexts: chunks and single tokens of some of them come in parts."""
+    rng = np.random.default_rng(count)
+    new = rng.choice(new, size=count)
+    lens = new + rng.integers(0, 3500, size=count) * (rng.random(count) < 0.3)
+    b = Batch(new, lens, 2, 1, 64, dtype, page, seed=32, **mask)
+    b.check(*b.attend())
+
+
 @pytest.mark.parametrize("page", [24, 64])
 @pytest.mark.parametrize("mask", [dict(), dict(causal=False, window=700, n_sink=64), dict(window=500)])
 def test_long_chunks_of_many_heads(page, mask):
