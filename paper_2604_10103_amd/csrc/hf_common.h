@@ -65,6 +65,13 @@ __device__ __forceinline__ float phi_apply(float x, int kind) {
   return x > 0.0f ? x + 1.0f : __expf(x);
 }
 
+// The largest of three scores, NaN if one is: one v_maximum3_f32, while fmaxf costs an instruction more per operand that may be a NaN.
+// Not inline assembly: scores come from matrix products, whose results are there 12 issue slots after the last one; the compiler counts
+// them for readers that it knows, and for no others.
+__device__ __forceinline__ float max_of3(float a, float b, float c) {
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
+}
+
 __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, kWave));

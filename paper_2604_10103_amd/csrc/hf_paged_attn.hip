@@ -48,15 +48,6 @@ template <int D> __device__ __forceinline__ int v_swizzle(int r) {
   return D == 128 ? ((r & 3) << 2 | ((r >> 2) & 3)) : (((r >> 1) & 1) << 2 | ((r >> 2) & 3));
 }
 
-// max without the quieting of NaNs around fmaxf: a NaN score makes its row's sum one in any case.  (Between the products that write the
-// scores and this, which the compiler does not know to read them, lie the reads of the next fragments: more than the 11 issue slots that
-// the results take.)
-__device__ __forceinline__ float max3f(float a, float b, float c) {
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
-}
-
 template <int D, int NW, int KS> struct Shape {
   static constexpr int BM = 32 * NW, NT = 64 * NW * KS;
   static constexpr int ROWB = 2 * D, TILE = kKeyTile * ROWB;
@@ -340,11 +331,12 @@ __global__ __launch_bounds__(64 * NW * KS, (NW > 1 ? 2 : 1)) void paged_attn_ker
         seen = 1;
       }
       // ---- online softmax in the exp2 domain
-      float mx = max3f(max3f(max3f(sacc[0], sacc[1], sacc[2]), max3f(sacc[3], sacc[4], sacc[5]), max3f(sacc[6], sacc[7], sacc[8])),
-                       max3f(sacc[9], sacc[10], sacc[11]), max3f(sacc[12], sacc[13], max3f(sacc[14], sacc[15], sacc[15])));
+      // (a row with a NaN keeps its reference: its sum is NaN in any case)
+      float mx = max_of3(max_of3(max_of3(sacc[0], sacc[1], sacc[2]), max_of3(sacc[3], sacc[4], sacc[5]), max_of3(sacc[6], sacc[7], sacc[8])),
+                         max_of3(sacc[9], sacc[10], sacc[11]), max_of3(sacc[12], sacc[13], max_of3(sacc[14], sacc[15], sacc[15])));
       {
         const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-        mx = max3f(__uint_as_float(sw[0]), __uint_as_float(sw[1]), __uint_as_float(sw[1])) * a.c_scale;
+        mx = max_of3(__uint_as_float(sw[0]), __uint_as_float(sw[1]), __uint_as_float(sw[1])) * a.c_scale;
       }
       // every row by its own maximum: what the other rows of the wavefront see is nothing to it
       const bool grows = mx > m_ref + kGrow;
