@@ -49,11 +49,6 @@ constexpr float kGrow = 8.0f;     // log2 units: rescale only when a row's maxim
 __device__ __forceinline__ int k_swizzle(int r) { return ((r >> 1) & 1) | (((r >> 2) ^ (r >> 3)) & 1) << 1 | (((r >> 3) ^ (r >> 4)) & 1) << 2; }
 __device__ __forceinline__ int v_swizzle(int r) { return ((r >> 1) & 1) << 2 | ((r >> 2) & 3); }
 
-__device__ __forceinline__ float max3f(float a, float b, float c) {   // (scores are finite or -inf: no NaN quieting)
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
-}
 __device__ __forceinline__ float both_halves_sum(float x) {
   const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
@@ -205,12 +200,12 @@ __global__ __launch_bounds__(128 * KS, 4) void attn_d64_kernel(
     }
     float mx;
     {
-      const float m0 = max3f(sacc[0], sacc[1], sacc[2]), m1 = max3f(sacc[3], sacc[4], sacc[5]);
-      const float m2 = max3f(sacc[6], sacc[7], sacc[8]), m3 = max3f(sacc[9], sacc[10], sacc[11]);
-      const float m4 = max3f(sacc[12], sacc[13], sacc[14]), m5 = max3f(m0, m1, m2);
-      mx = max3f(max3f(m3, m4, sacc[15]), m5, m5);
+      const float m0 = max_of3(sacc[0], sacc[1], sacc[2]), m1 = max_of3(sacc[3], sacc[4], sacc[5]);
+      const float m2 = max_of3(sacc[6], sacc[7], sacc[8]), m3 = max_of3(sacc[9], sacc[10], sacc[11]);
+      const float m4 = max_of3(sacc[12], sacc[13], sacc[14]), m5 = max_of3(m0, m1, m2);
+      mx = max_of3(max_of3(m3, m4, sacc[15]), m5, m5);
       const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-      mx = max3f(__uint_as_float(sw[0]), __uint_as_float(sw[1]), __uint_as_float(sw[1])) * c_scale;  // both lanes of a query agree
+      mx = max_of3(__uint_as_float(sw[0]), __uint_as_float(sw[1]), __uint_as_float(sw[1])) * c_scale;  // both lanes of a query agree
     }
     if (__any(mx > m_ref + kGrow)) {   // (any reference is exact in floating point)
       const float m_new = fmaxf(m_ref, mx);

@@ -56,19 +56,6 @@ constexpr float kRescaleThreshold = 8.0f;  // log2 units: rescale only when a ro
 // History branch fused into the epilogue (kFused): planes = the fp32 state split into two bf16
 // planes (hi, lo), transposed (Lt[plane][j][i], see hf_readout_mfma.hip), of which the first
 // n_planes are used; zvec = the state's normaliser.
-// max without the NaN-quieting canonicalisation the compiler adds around fmaxf (scores are finite
-// or -inf here): one instruction per three inputs
-__device__ __forceinline__ float max3f(float a, float b, float c) {
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
-}
-__device__ __forceinline__ float max2f(float a, float b) {
-  float r;
-  asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
-  return r;
-}
-
 struct HistArgs {
   const bf16_t* planes;  // [BH][2][d][d]
   const float* zvec;     // [BH][d]
@@ -985,7 +972,7 @@ __global__ __launch_bounds__(64 * NW * KS, 2) void attn_mfma_kernel(
   };
   auto row_max = [&](float mx) {   // of the lane's maximum; both lanes of a query agree
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-    return max2f(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * c_scale;
+    return max_of3(__uint_as_float(sw[0]), __uint_as_float(sw[1]), __uint_as_float(sw[1])) * c_scale;
   };
   // The first reference of a row is the maximum of the list's first tile in every group, as it is with one group: P is rounded
   // to bf16 against it, so an output does not depend on the number of groups but for the order of its fp32 sums.  (Each group
@@ -999,7 +986,7 @@ __global__ __launch_bounds__(64 * NW * KS, 2) void attn_mfma_kernel(
     for (int s = 0; s < 8; ++s)
       head = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(smem + k_addr[s]), qf[s], head, 0, 0, 0);
     mask_tile(head, __builtin_amdgcn_readfirstlane(valid_head));
-    float mx = head[0];   // (not max3f: the compiler has to see who reads an MFMA's result this soon, to wait for it)
+    float mx = head[0];
 #pragma unroll
     for (int r = 1; r < 16; ++r) mx = fmaxf(mx, head[r]);
     m_ref = row_max(mx);
@@ -1052,10 +1039,11 @@ __global__ __launch_bounds__(64 * NW * KS, 2) void attn_mfma_kernel(
     // ---- online softmax in the exp2 domain; statistics are per lane (= per query)
     float mx;
     {
-      const float m0 = max3f(sacc[0], sacc[1], sacc[2]), m1 = max3f(sacc[3], sacc[4], sacc[5]);
-      const float m2 = max3f(sacc[6], sacc[7], sacc[8]), m3 = max3f(sacc[9], sacc[10], sacc[11]);
-      const float m4 = max3f(sacc[12], sacc[13], sacc[14]);
-      mx = row_max(max2f(max3f(m0, m1, m2), max3f(m3, m4, sacc[15])));
+      const float m0 = max_of3(sacc[0], sacc[1], sacc[2]), m1 = max_of3(sacc[3], sacc[4], sacc[5]);
+      const float m2 = max_of3(sacc[6], sacc[7], sacc[8]), m3 = max_of3(sacc[9], sacc[10], sacc[11]);
+      const float m4 = max_of3(sacc[12], sacc[13], sacc[14]);
+      const float m5 = max_of3(m0, m1, m2);
+      mx = row_max(max_of3(max_of3(m3, m4, sacc[15]), m5, m5));
     }
     // lazy rescale: keep the reference max unless some row's max grew by more than the threshold
     if (__any(mx > m_ref + kRescaleThreshold)) {
