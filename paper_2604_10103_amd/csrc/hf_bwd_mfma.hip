@@ -447,6 +447,9 @@ __device__ __forceinline__ void dq_rows(
         __builtin_amdgcn_sched_barrier(0);
       }
       outlive(sn, dn);
+      // nor may what the products of dP^T start from: behind the last trip's first one, which reads it for seven slots, its registers
+      // would go to vector work
+      asm volatile("" :: "v"(dinit));
     };
     // slot numbers are literals, hence four trips per turn of the loop; the last one to three tiles take two or
     // four more trips (a tile past the list is zeros)
