@@ -609,7 +609,8 @@ HF_API int hf_rope_axes_apply(const hf_rope_axes* rope, int32_t dtype, int32_t h
  *               the packed operands.  A sequence may have none.  Rows from cu_new[n_seqs] on are neither read into anything nor written.
  *   seq_lens    device int32 [n_seqs]: tokens of every sequence, the new ones INCLUDED: new token i of a sequence with m of them and
  *               length n is token n - m + i (its place).  Tokens at a negative place or behind max_pages * page_tokens do not exist.
- * All lengths and tables are read on the device: a captured call follows what they hold when it is replayed.
+ * All lengths and tables are read on the device: a captured call follows what they hold when it is replayed.  Nothing that a call writes
+ * (pages, outputs, workspace) may lie over them or over its positions.
  *
  * Packed operands are [rows, heads, head_dim] with head_dim contiguous; their strides arguments are HOST int64 [2], distances between
  * rows and between heads in elements, multiples of 16 bytes (a view into the rows of a joint projection); NULL: contiguous. */

@@ -121,6 +121,18 @@ bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
   return x < y + nb && y < x + na;
 }
 
+// What the call writes must not lie over what its later workgroups read
+int check_reads(const void* written, int64_t bytes, const char* name, const hf_paged& c, const int32_t* cu_new, const int32_t* seq_lens,
+                const int32_t* page_table, const int32_t* positions = nullptr, int64_t n_positions = 0) {
+  const struct { const int32_t* p; int64_t n; const char* name; } reads[] = {{cu_new, (int64_t)c.n_seqs + 1, "cu_new"},
+                                                                             {seq_lens, c.n_seqs, "seq_lens"},
+                                                                             {page_table, (int64_t)c.n_seqs * c.max_pages, "page_table"},
+                                                                             {positions, n_positions, "positions"}};
+  for (const auto& r : reads)
+    if (r.p && overlap(written, bytes, r.p, 4 * r.n)) { set_error("%s overlaps %s", name, r.name); return HF_ERR_SHAPE; }
+  return HF_OK;
+}
+
 int64_t pool_bytes(const hf_paged& c) {
   return (int64_t)c.n_pages * c.heads_kv * c.page_tokens * c.head_dim * (c.dtype == HF_BF16 ? 2 : 4);
 }
@@ -208,6 +220,10 @@ int hf_paged_append(const hf_paged* cache, const hf_rope_axes* rope_or_null, int
       set_error("%s overlaps the pages", x == &k ? "K_new" : "V_new");
       return HF_ERR_SHAPE;
     }
+  const int32_t* read = rope_or_null ? positions : nullptr;
+  const int64_t n_read = rope_or_null ? (int64_t)rope_or_null->n_axes * n_new : 0;
+  HF_TRY(check_reads(K_pages, pool, "K_pages", *cache, cu_new, seq_lens, page_table, read, n_read));
+  HF_TRY(check_reads(V_pages, pool, "V_pages", *cache, cu_new, seq_lens, page_table, read, n_read));
   if (Q_or_null) {
     HF_TRY(check_packed(q, Q_or_null, "Q", q_strides, false));
     HF_TRY(check_packed(o, Q_out, "Q_out", q_out_strides, true));
@@ -217,6 +233,7 @@ int hf_paged_append(const hf_paged* cache, const hf_rope_axes* rope_or_null, int
         set_error("%s overlaps the pages", x == &q ? "Q" : "Q_out");
         return HF_ERR_SHAPE;
       }
+    HF_TRY(check_reads(o.p, o.span(), "Q_out", *cache, cu_new, seq_lens, page_table, read, n_read));
   }
   return launch_paged_append(*cache, rope_or_null, n_new, K_new, k.stride, V_new, v.stride, Q_or_null, q.stride, cu_new, seq_lens, positions,
                              K_pages, V_pages, page_table, Q_out, o.stride, static_cast<hipStream_t>(stream));
@@ -243,6 +260,7 @@ int hf_paged_attn_fwd(const hf_paged* cache, const void* Q, const int64_t* q_str
   HF_TRY(check_apart(q, o, "O overlaps Q", false));
   const int64_t pool = pool_bytes(*cache), lse = lse2_or_null ? (int64_t)cache->heads * n_q * 4 : 0;
   if (overlap(o.p, o.span(), K_pages, pool) || overlap(o.p, o.span(), V_pages, pool)) { set_error("O overlaps the pages"); return HF_ERR_SHAPE; }
+  HF_TRY(check_reads(o.p, o.span(), "O", *cache, cu_new, seq_lens, page_table));
   if (lse2_or_null) {
     HF_TRY(check_ptr(lse2_or_null, "lse2", 4));
     if (overlap(o.p, o.span(), lse2_or_null, lse) || overlap(q.p, q.span(), lse2_or_null, lse) || overlap(K_pages, pool, lse2_or_null, lse) ||
@@ -250,6 +268,7 @@ int hf_paged_attn_fwd(const hf_paged* cache, const void* Q, const int64_t* q_str
       set_error("lse2 overlaps another argument");
       return HF_ERR_SHAPE;
     }
+    HF_TRY(check_reads(lse2_or_null, lse, "lse2", *cache, cu_new, seq_lens, page_table));
   }
   const size_t need = paged_workspace_bytes(*cache, n_q);
   if (need) {
@@ -264,6 +283,7 @@ int hf_paged_attn_fwd(const hf_paged* cache, const void* Q, const int64_t* q_str
       set_error("workspace overlaps another argument");
       return HF_ERR_SHAPE;
     }
+    HF_TRY(check_reads(workspace, w, "workspace", *cache, cu_new, seq_lens, page_table));
   }
   PagedAttnArgs a = {};
   a.Q = Q;
