@@ -649,7 +649,8 @@ HF_API int hf_paged_workspace_bytes(const hf_paged* cache, int32_t n_q, size_t* 
 /* Attention of every sequence's new tokens over its pages (their own keys and values have been appended before):
  *     O = sum_j softmax_j(softmax_scale q . k_j) v_j   over the keys j that the token sees (causal, window, n_sink of the cache)
  * One token a sequence (decoding), a few, or whole chunks; sequences of both kinds in one call.
- *   Q, O      packed [n_q, heads, head_dim], n_q * heads <= 2^30; O must not overlap Q, and its rows may not overlap each other
+ *   Q, O      packed [n_q, heads, head_dim], n_q * heads <= 2^30; O must not overlap Q, and its rows may not overlap each other.  A launch
+ *             has less than 2^32 threads: n_q * heads / 128 + n_seqs * heads_kv up to 2^22 always fit, more are refused where they do not
  *   lse2_or_null  out fp32 [heads, n_q]: log2 of the softmax denominator, logits scaled by softmax_scale * log2(e), as
  *             hf_hybrid_attn_fwd_save writes it: parts of an attention over several caches can be joined by it
  *   workspace >= hf_paged_workspace_bytes(cache, n_q) bytes, 256-byte aligned, no initialisation needed; two calls that may overlap in

@@ -65,6 +65,7 @@ int check_cache(const hf_paged* c) {
 int check_attn_rows(const hf_paged* c, int32_t n_q) {
   HF_TRY(check_rows(n_q, "n_q"));
   if ((int64_t)n_q * c->heads > (1ll << 30)) { set_error("n_q * heads must be <= 2^30"); return HF_ERR_SHAPE; }
+  if (n_q > 0 && paged_threads(*c, n_q) >= (1ll << 32)) { set_error("more rows and sequences than a launch of 2^32 threads holds"); return HF_ERR_SHAPE; }
   return HF_OK;
 }
 

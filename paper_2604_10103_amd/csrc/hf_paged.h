@@ -27,6 +27,7 @@ struct PagedAttnArgs {
   uint32_t group_magic;
   int group_shift;
 };
+long long paged_threads(const hf_paged& c, int n_q);   // of the launch; 2^32 are too many
 size_t paged_workspace_bytes(const hf_paged& c, int n_q);
 int launch_paged_attn(const hf_paged& c, PagedAttnArgs a, void* workspace, hipStream_t s);
 struct PagedSchedule;

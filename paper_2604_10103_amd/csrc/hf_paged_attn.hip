@@ -554,6 +554,11 @@ template <int D> int launch_of(const PagedAttnArgs& a, const PagedSchedule& sc, 
 
 }  // namespace
 
+long long paged_threads(const hf_paged& c, int n_q) {
+  const Plan p = plan_of(c, n_q);
+  return (long long)p.grid * (2 * p.rows * p.ks);   // 64 for 32 rows, times the groups
+}
+
 size_t paged_workspace_bytes(const hf_paged& c, int n_q) {
   if (n_q == 0) return 0;
   const Plan p = plan_of(c, n_q);

@@ -53,3 +53,27 @@ def test_attention_does_not_write_over_lengths_and_tables(read):
         for at in (into, into + size - 4, into - READS[read] + 4):
             assert _attend(lib, **{read: at}) == -2
             assert b"overlaps" in lib.hf_last_error()
+
+
+def _large(n_seqs, heads, heads_kv, head_dim=64, dtype="bf16"):
+    return hf.make_paged(heads=heads, heads_kv=heads_kv, head_dim=head_dim, dtype=dtype, page_tokens=64, n_pages=1000, n_seqs=n_seqs, max_pages=8)
+
+
+@pytest.mark.parametrize("n_seqs,new,heads,heads_kv,head_dim,dtype", [(65535, 33, 256, 256, 64, "bf16"), (65535, 33, 256, 256, 128, "f32"),
+                                                                     (65535, 40, 400, 400, 128, "bf16")])
+def test_more_workgroups_than_a_launch_has(n_seqs, new, heads, heads_kv, head_dim, dtype):
+    """2^32 threads or more: refused by both calls alike, before anything else is looked at."""
+    lib, c, n = hf.load(), _large(n_seqs, heads, heads_kv, head_dim, dtype), n_seqs * new
+    assert n * heads <= 1 << 30 and (n * heads // 128 + n_seqs * heads_kv) * 256 >= 1 << 32
+    with pytest.raises(hf.HFError, match="threads") as e:
+        hf.hf_paged_workspace_bytes(c, n)
+    assert e.value.code == -2
+    assert lib.hf_paged_attn_fwd(ctypes.byref(c), None, None, n, CU, LENS, KP, VP, TABLE, OUT, None, None, None, 0, None) == -2
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("head_dim", [64, 128])
+@pytest.mark.parametrize("n_seqs,n,heads,heads_kv", [(1, 1 << 22, 256, 256), (1, 1 << 24, 64, 1), (65535, 65535, 16384, 16384), (65535, 65535 * 33, 64, 32),
+                                                     (1, 0, 65535, 65535)])
+def test_large_calls_that_a_launch_can_hold(n_seqs, n, heads, heads_kv, head_dim, dtype):
+    hf.hf_paged_workspace_bytes(_large(n_seqs, heads, heads_kv, head_dim, dtype), n)
