@@ -652,7 +652,8 @@ HF_API int hf_paged_workspace_bytes(const hf_paged* cache, int32_t n_q, size_t* 
  *   Q, O      packed [n_q, heads, head_dim], n_q * heads <= 2^30; O must not overlap Q, and its rows may not overlap each other.  A launch
  *             has less than 2^32 threads: n_q * heads / 128 + n_seqs * heads_kv up to 2^22 always fit, more are refused where they do not
  *   lse2_or_null  out fp32 [heads, n_q]: log2 of the softmax denominator, logits scaled by softmax_scale * log2(e), as
- *             hf_hybrid_attn_fwd_save writes it: parts of an attention over several caches can be joined by it
+ *             hf_hybrid_attn_fwd_save writes it.  Parts of an attention over several caches are joined by it, with weights 2^(lse2 - the
+ *             largest): +inf stands for a part without a key, which has the weight 0 and does not count for the largest
  *   workspace >= hf_paged_workspace_bytes(cache, n_q) bytes, 256-byte aligned, no initialisation needed; two calls that may overlap in
  *             time must not share one
  * A token that sees no key gets O = 0 and lse2 = +inf.  What a token does not see, it does not depend on, a NaN or an infinity
