@@ -591,7 +591,8 @@ typedef struct hf_rope_axes {
  *              otherwise the two address ranges must be disjoint.
  *   positions  device int32 [n_axes, n_tokens] for all batches, or, positions_per_batch != 0, [batch, n_axes, n_tokens]; any value
  *   n_tokens   0 is allowed: nothing is enqueued
- * Angles are reduced in 64 bits; sine, cosine and the products are fp32 (the first two off by 2.5 units of 2^-24 at most), with one rounding to dtype. */
+ * Angles are reduced in 64 bits and what these leave of rate and product; sine, cosine and the products are fp32 (the first two off by
+ * 2.5 units of 2^-24 at most, whatever the position), with one rounding to dtype. */
 HF_API int hf_rope_axes_apply(const hf_rope_axes* rope, int32_t dtype, int32_t head_dim, int32_t batch, int32_t heads, int32_t n_tokens,
                   const void* X, const int64_t* x_strides, const int32_t* positions, int32_t positions_per_batch,
                   void* Y, const int64_t* y_strides, int32_t inverse, void* stream);

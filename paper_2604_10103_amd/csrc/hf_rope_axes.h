@@ -9,7 +9,8 @@ constexpr int kMaxPairs = 64;   // head_dim / 2
 
 // by value in the kernels' arguments
 struct AxesSpec {
-  double quarter[kMaxPairs];   // quarter turns per position step of every pair
+  double quarter[kMaxPairs];   // quarter turns per position step of every pair,
+  float rest[kMaxPairs];       // and what rounding to 64 bits left of them
   uint32_t axis[4];            // two bits a pair: its axis
   int pairs;                   // P
   int n_axes;
@@ -25,18 +26,19 @@ enum AxesMode {
 template <int D, int MODE> constexpr int axes_features() { return MODE == kAdjacent ? 8 : 16; }             // of a thread
 template <int D, int MODE> constexpr int axes_threads() { return D / axes_features<D, MODE>(); }            // of a row
 
-// cos and sin of pos * quarter quarter turns.  The product and its reduction to [-1/2, 1/2] quarter turns are formed in 64 bits (a
-// position of 2^31 leaves 2^-22 of a radian there; in 32 bits one of 2^16 would leave 2^-8), what is left goes through the Taylor
-// polynomials of degree 9 and 10, whose next terms are 1.8e-9 and 1.2e-10 at pi/4.
-__device__ __forceinline__ void quarter_turns(double quarter, int pos, float& c, float& s) {
-  const double t = (double)pos * quarter, q = rint(t);
-  const float a = (float)((t - q) * 1.57079632679489661923), a2 = a * a;
+// cos and sin of pos * (quarter + rest) quarter turns.  In 64 bits the product alone would be off by 2^-22 of a radian at a position of
+// 2^31, and so would the rate's rounding be: the whole quarter turns are taken from the product before it is rounded, and the rate's rest
+// is added (in 32 bits a position of 2^16 would leave 2^-8).  What is left, [-1/2, 1/2] quarter turns, goes through the Taylor polynomials
+// of degree 9 and 10, whose next terms are 1.8e-9 and 1.2e-10 at pi/4: 1.2 units of 2^-24 in all, at any position.
+__device__ __forceinline__ void quarter_turns(double quarter, float rest, int pos, float& c, float& s) {
+  const double x = (double)pos, q = rint(x * quarter), part = fma(x, (double)rest, fma(x, quarter, -q));
+  const float a = (float)(part * 1.57079632679489661923), a2 = a * a;
   const int k = (int)q;   // (theta >= 1: below 2^31)
   const float sp = a * fmaf(a2, fmaf(a2, fmaf(a2, fmaf(a2, 1.0f / 362880.0f, -1.0f / 5040.0f), 1.0f / 120.0f), -1.0f / 6.0f), 1.0f);
   const float cp = fmaf(a2, fmaf(a2, fmaf(a2, fmaf(a2, fmaf(a2, -1.0f / 3628800.0f, 1.0f / 40320.0f), -1.0f / 720.0f), 1.0f / 24.0f), -0.5f), 1.0f);
-  const float x = (k & 1) ? sp : cp, y = (k & 1) ? cp : sp;
-  c = ((k + 1) & 2) ? -x : x;
-  s = (k & 2) ? -y : y;
+  const float u = (k & 1) ? sp : cp, v = (k & 1) ? cp : sp;
+  c = ((k + 1) & 2) ? -u : u;
+  s = (k & 2) ? -v : v;
 }
 
 // the angles of thread g of a token: 4 pairs (kAdjacent) or 8
@@ -49,14 +51,18 @@ template <int D, int MODE> struct Angles {
 #pragma unroll
     for (int a = 0; a < HF_ROPE_MAX_AXES; ++a) pos[a] = a < spec.n_axes ? at(a) : 0;
     double quarter[N];
+    float rest[N];
     uint32_t axis = spec.axis[(N * g) >> 4] >> (2 * ((N * g) & 15));   // (N pairs lie in one word)
 #pragma unroll
-    for (int i = 0; i < N; ++i) quarter[i] = spec.quarter[N * g + i];
+    for (int i = 0; i < N; ++i) {
+      quarter[i] = spec.quarter[N * g + i];
+      rest[i] = spec.rest[N * g + i];
+    }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int ax = (axis >> (2 * i)) & 3;
       const int p = ax < 2 ? (ax == 0 ? pos[0] : pos[1]) : (ax == 2 ? pos[2] : pos[3]);
-      quarter_turns(quarter[i], p, c[i], s[i]);
+      quarter_turns(quarter[i], rest[i], p, c[i], s[i]);
       if (flip) s[i] = -s[i];
     }
   }
@@ -201,18 +207,28 @@ __device__ __forceinline__ void copy_rows(int g, int i0, int i1, From from, To t
   }
 }
 
-// host
+// host.  A spectrum's rates are powers of one ratio, formed by products of 64 bits' precision: the 63rd is off by 2^-57 of itself, which
+// a position of 2^31 makes a third of 2^-24 (a powl for each of 64 takes some microseconds of every call)
 inline AxesSpec axes_spec(const hf_rope_axes& r) {
   AxesSpec s = {};
   s.n_axes = r.n_axes;
   for (int a = 0; a < r.n_axes; ++a) s.pairs += r.pairs[a];
+  constexpr long double kTurn = 0.636619772367581343075535053490057448L;   // 2 / pi
+  const auto ratio_of = [&](int n) { return powl((long double)r.theta, -1.0L / n); };
+  long double quarter = kTurn, ratio = ratio_of(s.pairs);
   int p = 0;
-  for (int a = 0; a < r.n_axes; ++a)
-    for (int i = 0; i < r.pairs[a]; ++i, ++p) {
-      const double power = r.spectrum == HF_ROPE_SHARED ? (double)p / s.pairs : (double)i / r.pairs[a];
-      s.quarter[p] = pow(r.theta, -power) * 0.63661977236758134308;   // 2 / pi
-      s.axis[p >> 4] |= (uint32_t)a << (2 * (p & 15));
+  for (int a = 0; a < r.n_axes; ++a) {
+    if (r.spectrum == HF_ROPE_PER_AXIS) {
+      quarter = kTurn;
+      ratio = ratio_of(r.pairs[a]);
     }
+    for (int i = 0; i < r.pairs[a]; ++i, ++p) {
+      s.quarter[p] = (double)quarter;
+      s.rest[p] = (float)(quarter - s.quarter[p]);
+      s.axis[p >> 4] |= (uint32_t)a << (2 * (p & 15));
+      quarter *= ratio;
+    }
+  }
   return s;
 }
 
