@@ -18,10 +18,10 @@
 //           costs; each of `groups` workgroups gets an equal share of the line.  A share's end that falls near a row tile's ends moves
 //           there.  So a workgroup has whole row tiles and at most two parts.
 // Where workgroups of 32 rows have work for more than one round, shares are taken if the model expects them to be faster: 64 single
-// tokens over 500 to 8191 keys 210 us, in pieces 278.  Rows of chunks read the same keys at the same time when they lie in pieces, and
+// tokens over 500 to 8191 keys 211 us, in pieces 278.  Rows of chunks read the same keys at the same time when they lie in pieces, and
 // find them in the L2; in shares they do not (4680 rows of 12 heads over 9360 keys take an eighth longer).  Nor does it pay to cut off
-// what the longest rows have over the others: 4680 rows that see 10920 to 14040 keys 405 us whole, 429 to 451 with 14 to 22 % cut off.
-// A single token over 4096 keys takes 14.8 us in parts, 34.4 whole; one over 131071 keys (four rows) 114 and 1130.
+// what the longest rows have over the others: 4680 rows that see 10920 to 14040 keys take 6 to 11 % longer with 14 to 22 % of these cut off.
+// A single token over 4096 keys takes 15 us in parts, 34 whole; four over 131071 keys 108 and 1130.
 //
 // Parts of a row meet in the workspace: each writes its sums (fp32) there, the last one to arrive adds them in the order of the parts.
 #pragma once
@@ -297,7 +297,7 @@ template <int BM, bool kShares> __device__ __forceinline__ PagedWork find_work(c
 }
 
 // What both ways have in common: the sequence that holds place y, and what precedes it.  The 64 sequences that are looked at stay: a workgroup's
-// next item is among them or behind, but for another head's (2048 single tokens over 3 to 60 keys 1096 us when every item began at the first, then 618)
+// next item is among them or behind, but for another head's (2048 single tokens over 3 to 60 keys 1096 us when every item began at the first, then 618; by a wavefront each 332)
 template <int BM> __device__ __forceinline__ bool find_seq(const PagedAttnArgs& a, const PagedSchedule& sc, const PagedWork& p, int y, SeqBlock& block,
                                                           SeqWork& q, int& seq, int& before, int& split_before) {
   const int lane = thread_id() & 63;

@@ -5,10 +5,11 @@
 // so that the statistics of a row are private to its two lanes and the exponentials of S^T are, rounded to bf16, the B operand of the
 // second product (that rounding, half a step of each probability, averages out over the keys: outputs are 0.0023 off 64 bits where exact
 // probabilities leave 0.0017, the output's own rounding; a product of the remainders would double the second half of the matrix work).
-// K and V tiles go global -> LDS directly, V^T fragments are transposing reads, three K slots and two V slots.
+// K and V tiles go global -> LDS directly, V^T fragments are transposing reads, three K slots (four where wavefronts share tiles) and two V
+// slots.
 // Here the rows are tokens x heads of a group, and a tile lies in a page.  A wavefront finds out for 64 tiles at once where they lie, a lane
-// each; a tile's descriptor is then a few scalar instructions.  (12 heads x 4680 x 9360, pages of 1560: 279 us, with an address for every
-// lane instead 322.  Entries of the table that the scalar unit reads a tile ahead cost a sixth: they are on their way when the tile's
+// each; a tile's descriptor is then a few scalar instructions.  (12 heads x 4680 x 9360, pages of 1560: 287 us, with an address for every
+// lane instead, as for pages of 16, 334; prompts of 2048 tokens over 6100 314 and 429.  Entries of the table that the scalar unit reads a tile ahead cost a sixth: they are on their way when the tile's
 // barrier waits for everything that is; tiles that go on in the next page, and a branch for them, a tenth.)
 //
 // Four shapes of workgroup (NW wavefronts of rows, KS groups of wavefronts that share the keys):
@@ -17,10 +18,10 @@
 //   NW 1, KS 4   32 rows, every wavefront its own tiles and no barrier until the end: single tokens
 //   NW 1, KS 1   the same by one wavefront, four workgroups a compute unit: single tokens of many sequences
 // The first two are bound by matrix cores and softmax together, whose instructions a SIMD's two wavefronts issue one after the other, and by
-// power: 12 heads x 4680 x 9360 reach 966 TFLOP/s at the 2.0 GHz that the chip holds there, the matrix cores 44 % of the cycles busy, the
-// vector units 43 %, no LDS conflict.  (Wavefronts that take turns between barriers, one half at the products while the other is at its
-// exponentials, need 360 us for 266: alone, a wavefront leaves a fifth of the vector unit's issue slots empty.)  The others are bound by
-// memory: 64 single tokens over 500 to 8191 keys in 210 us, 5.6 TB/s; short ones by the chain arguments, lengths, page table, keys
+// power: 12 heads x 4680 x 9360 reach 940 TFLOP/s at the 1.9 to 2.0 GHz that the chip holds there, the matrix cores 44 % of the cycles busy,
+// the vector units 43 %, no LDS conflict.  (Wavefronts that take turns between barriers, one half at the products while the other is at its
+// exponentials, need a third longer: alone, a wavefront leaves a fifth of the vector unit's issue slots empty.)  The others are bound by
+// memory: 64 single tokens over 500 to 8191 keys in 211 us, 5.6 TB/s; short ones by the chain arguments, lengths, page table, keys
 // (118 keys: 8.4 us, of which 3.3 go until the work is known, 1.5 until the rows are there, 1.4 for a tile, 1.0 for the end).
 #include "hf_paged_attn.h"
 
@@ -464,8 +465,8 @@ Plan plan_of(const hf_paged& c, int n_q) {
   Plan p = {};
   auto tiles = [&](int of) { return (rows / of + (n_q < c.n_seqs ? n_q : c.n_seqs)) * c.heads_kv; };   // row tiles of all heads, at most
   // A workgroup of 128 rows where a sequence has more than 32 on the average.  256 rows, whose tiles travel half as often, take 0.89 us a
-  // tile where two workgroups of 128 take 1.07, if a compute unit's rounds of them are no more (12 heads x 4680 x 9360: 279 and 293 us;
-  // a prompt of 4096, 32 heads on 8: 156 and 161).  The times are fits to launches of 128 to 768 row tiles over 256 to 4096 keys.
+  // tile where two workgroups of 128 take 1.07, if a compute unit's rounds of them are no more (12 heads x 4680 x 9360: 287 and 293 us;
+  // over a window of 9360 and a sink frame 415 and 430; a prompt of 4096, 32 heads on 8: 157 and 158).  The times are fits to launches of 128 to 768 row tiles over 256 to 4096 keys.
   p.rows = rows > 32ll * c.n_seqs ? 128 : 32;
   if (p.rows == 128 && c.dtype == HF_BF16 && c.head_dim == 128 && rows > 128ll * c.n_seqs) {
     const long long n = (rows + c.n_seqs - 1) / c.n_seqs, heads = (long long)c.n_seqs * c.heads_kv;   // (as if all were as long)
@@ -475,7 +476,7 @@ Plan plan_of(const hf_paged& c, int n_q) {
   p.ks = p.rows == 32 ? 4 : 1;
   p.sc.units = 256.0f;
   // A row tile a wavefront where there are enough for all: its chain (rows, page table, first keys) then passes next to three others'.  512
-  // sequences of 13 to 250 keys, 8 key heads: 98 us, with four wavefronts a row tile 192; 256 of 150 to 3000: 308 and 305; 128 of 400 to
+  // sequences of 13 to 250 keys, 8 key heads: 100 us, with four wavefronts a row tile 192; 256 of 150 to 3000: 308 and 305; 128 of 400 to
   // 8000: 397 and 378
   if (p.rows == 32 && tiles(32) >= 1024) {
     p.ks = 1;

@@ -3,7 +3,7 @@
 // Both move every row once: they are bound by memory.  A thread owns the same few pairs of a token for many heads, so that an angle
 // (a product and a reduction in 64 bits, two polynomials: some fifty instructions) is formed once and serves them all.  10800 tokens of
 // 80 rows turn in 89 us, 5.0 TB/s; two streams' 4680 tokens of 12 keys, values and queries are appended in 42 us, 4.1 TB/s, of which some
-// 4 us are the launch and the chain lengths, page table, rows; a token of 40 rows turns in 4.7 us, 64 single tokens are appended in 5.4.
+// 4 us are the launch and the chain lengths, page table, rows; a token of 40 rows turns in 4 to 4.7 us, 64 single tokens are appended in 5.7.
 #include <math.h>
 
 #include <algorithm>

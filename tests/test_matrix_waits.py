@@ -135,7 +135,8 @@ def test_the_search_itself():
     assert [x[1:4] for x in too_early(jump)] == [("0x0", "0x10", 1)]
 
 
-@pytest.mark.parametrize("family", ["paged_attn_kernel", "attn_mfma_kernel", "attn_d64_kernel", "bwd_mfma_kernel"])
+@pytest.mark.parametrize("family", ["paged_attn_kernel", "attn_mfma_kernel", "attn_d64_kernel", "attn_split_kernel", "attn_w64_kernel", "bwd_mfma_kernel",
+                                    "absorb_quad_kernel", "absorb_mfma_kernel", "readout_mfma_kernel"])
 def test_results_of_products_are_waited_for(kernels, family):
     some = {n: code for n, code in kernels.items() if family in n and any(x[0] in PASSES for x in code)}
     assert some
