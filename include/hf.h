@@ -597,6 +597,56 @@ HF_API int hf_rope_axes_apply(const hf_rope_axes* rope, int32_t dtype, int32_t h
                   const void* X, const int64_t* x_strides, const int32_t* positions, int32_t positions_per_batch,
                   void* Y, const int64_t* y_strides, int32_t inverse, void* stream);
 
+/* ---- Norms of queries and keys, with the rotation in the same pass ---------------------------------------
+ * What a layer does to a head's row between its projection and attention: the row is brought to unit mean square, weighted, and turned
+ * by its token's positions.  The turn may be scaled for contexts longer than the trained one. */
+typedef struct hf_head_norm {
+  float   eps;         /* >= 0, finite */
+  int32_t per_head;    /* weights are 0: [head_dim], the same for all heads; else [heads, head_dim] */
+} hf_head_norm;
+
+/* A pair that makes t turns over `trained` positions (t = trained * rate / (2 pi)) turns at rate * (k + (1 - k) / factor) instead, with
+ * k = (t - slow) / (fast - slow), cut to [0, 1]: fast pairs keep their rate, slow ones are spread over a context `factor` times as long.
+ * Cosine and sine are multiplied by `amplitude` (the turned features only). */
+typedef struct hf_rope_scaling {
+  double  factor;      /* >= 1, finite */
+  double  trained;     /* > 0, finite */
+  double  slow, fast;  /* 0 <= slow < fast, finite */
+  float   amplitude;   /* > 0, finite */
+  int32_t axes;        /* bit a: the rates of axis a are scaled (a video's time may get long, its rows and columns do not) */
+} hf_rope_scaling;
+
+/* Y = A R(p) (w . x r),  r = 1 / sqrt(mean(x^2) + eps), for every row x: w the weights, R(p) the turn of hf_rope_axes_apply by the token's
+ * positions, A the scaling's amplitude on the turned features.
+ *   norm       NULL: no norm (r = 1, no weights);  rope  NULL: no turn (positions, scaling NULL too).  Not both.
+ *   scaling    NULL: none
+ *   X, Y, their strides, positions, n_tokens   as for hf_rope_axes_apply: strided rows, Y may be X, 0 tokens
+ *   weight     device fp32 as norm->per_head says, contiguous, NULL: ones; not over Y
+ * fp32 arithmetic with one rounding to dtype; squares are summed in fp32 (a row of values beyond 2^60 or of an infinity has no finite
+ * norm, a row of zeros with eps = 0 becomes NaN). */
+HF_API int hf_norm_rope_fwd(const hf_head_norm* norm_or_null, const hf_rope_axes* rope_or_null, const hf_rope_scaling* scaling_or_null,
+                  int32_t dtype, int32_t head_dim, int32_t batch, int32_t heads, int32_t n_tokens, const void* X, const int64_t* x_strides,
+                  const float* weight_or_null, const int32_t* positions, int32_t positions_per_batch, void* Y, const int64_t* y_strides,
+                  void* stream);
+
+/* Bytes of scratch that hf_norm_rope_bwd needs for the gradient of the weights.  Host-only. */
+HF_API int hf_norm_rope_bwd_workspace_bytes(const hf_head_norm* norm, int32_t head_dim, int32_t batch, int32_t heads, int32_t n_tokens,
+                  size_t* bytes_out);
+
+/* Gradients of hf_norm_rope_fwd from its X and the gradient dY with respect to Y: with g = A R(-p) dY, u = x r,
+ *     dX = r (w . g - u mean(w . g . u)),    dweight = the sum of g . u over all rows that share the weights.
+ *   X, dY, dX  [batch, heads, n_tokens, head_dim], strides as above; strides of X and dY may be zero (one row for many), where dX still
+ *              gets the gradient of every place.  dX may be X or dY (the same address and strides), otherwise it overlaps neither
+ *   dweight_or_null  out fp32, the shape of the weights (also where `weight` is NULL: ones); norm given.  Written whole, zeros if there are
+ *              no tokens.  The sum is formed in fp32 in a fixed order: the same bits every time
+ *   workspace  for dweight: >= hf_norm_rope_bwd_workspace_bytes bytes, 256-byte aligned, no initialisation needed; NULL without dweight.
+ *              Two calls that may overlap in time must not share one */
+HF_API int hf_norm_rope_bwd(const hf_head_norm* norm_or_null, const hf_rope_axes* rope_or_null, const hf_rope_scaling* scaling_or_null,
+                  int32_t dtype, int32_t head_dim, int32_t batch, int32_t heads, int32_t n_tokens, const void* X, const int64_t* x_strides,
+                  const float* weight_or_null, const int32_t* positions, int32_t positions_per_batch, const void* dY,
+                  const int64_t* dy_strides, void* dX, const int64_t* dx_strides, float* dweight_or_null, void* workspace,
+                  size_t workspace_bytes, void* stream);
+
 /* ---- A cache of pages that many sequences share --------------------------------------------------------
  * The window calls above keep the keys and values of sequences of ONE length side by side.  Here a pool of pages of page_tokens tokens
  * each holds sequences (prompts, streams) of any lengths; a table names the pages of every sequence in order.  A page may be a latent
@@ -664,6 +714,40 @@ HF_API int hf_paged_workspace_bytes(const hf_paged* cache, int32_t n_q, size_t* 
 HF_API int hf_paged_attn_fwd(const hf_paged* cache, const void* Q, const int64_t* q_strides, int32_t n_q,
                   const int32_t* cu_new, const int32_t* seq_lens, const void* K_pages, const void* V_pages,
                   const int32_t* page_table, void* O, const int64_t* o_strides, float* lse2_or_null,
+                  void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- The cache of pages in 8 bits ---------------------------------------------------------------------------
+ * The pages of hf_paged, their keys and values as e4m3 (4 significant bits, 2^-9 .. 448) with a scale for each row:
+ *   K_pages, V_pages    [n_pages, heads_kv, page_tokens, head_dim] bytes, contiguous, 16-byte aligned
+ *   K_scales, V_scales  [n_pages, heads_kv, page_tokens] fp32, contiguous: a row stands for its codes times its scale
+ * cache->dtype is that of the packed operands.  Tables, lengths, places and masks are those of the calls above. */
+
+/* New keys, normalised and turned, and new values enter the pages; the queries of the same tokens are normalised and turned beside them.
+ * A row y (in fp32: no rounding to dtype in between) is written as
+ *     scale = max(max |y_f| * c, 2^-126),  c = 1 / 448 rounded to fp32;   code_f = y_f / scale, both rounded to nearest, ties to even,
+ * and a row with a NaN or an infinity as zeros with a scale of NaN: it reads as NaN.
+ *   norm      NULL: none; its per_head holds for both weights.  k_weight, q_weight: as hf_norm_rope_fwd's, NULL: ones
+ *   rope, scaling, positions, K_new, V_new, Q, Q_out, n_new   as for hf_paged_append and hf_norm_rope_fwd; values are only quantised.
+ *             Neither norm nor rope: keys are only quantised, queries copied
+ * What is written (pages, scales, Q_out) lies over nothing else that the call is given. */
+HF_API int hf_paged_append_e4m3(const hf_paged* cache, const hf_head_norm* norm_or_null, const hf_rope_axes* rope_or_null,
+                  const hf_rope_scaling* scaling_or_null, int32_t n_new, const void* K_new, const int64_t* k_strides, const void* V_new,
+                  const int64_t* v_strides, const void* Q_or_null, const int64_t* q_strides, const float* k_weight_or_null,
+                  const float* q_weight_or_null, const int32_t* cu_new, const int32_t* seq_lens, const int32_t* positions, void* K_pages,
+                  void* V_pages, float* K_scales, float* V_scales, const int32_t* page_table, void* Q_out, const int64_t* q_out_strides,
+                  void* stream);
+
+/* Bytes of scratch hf_paged_attn_e4m3_fwd needs for n_q packed rows, whatever the lengths are.  Host-only. */
+HF_API int hf_paged_e4m3_workspace_bytes(const hf_paged* cache, int32_t n_q, size_t* bytes_out);
+
+/* hf_paged_attn_fwd over pages in 8 bits: the same rows, masks, lse2, workspace rules and refusals.  Codes are multiplied as they are, a
+ * key's scale with its score and a value's with its probability, so that nothing of the cache is rounded again: fp32 scores, statistics
+ * and sums; in bf16 the product of probability and scale is rounded to bf16 for the second product.  What a token does not see, it does
+ * not depend on, codes and scales that are NaN or infinite included; a NaN that it sees (code or scale) makes the outputs that it enters
+ * NaN. */
+HF_API int hf_paged_attn_e4m3_fwd(const hf_paged* cache, const void* Q, const int64_t* q_strides, int32_t n_q,
+                  const int32_t* cu_new, const int32_t* seq_lens, const void* K_pages, const void* V_pages, const float* K_scales,
+                  const float* V_scales, const int32_t* page_table, void* O, const int64_t* o_strides, float* lse2_or_null,
                   void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---- Measurement helper (no part of the method) ------------------------------------------------ */

@@ -71,6 +71,15 @@ class hf_paged(ctypes.Structure):
                 ("causal", ctypes.c_int32), ("window", ctypes.c_int32), ("n_sink", ctypes.c_int32), ("softmax_scale", ctypes.c_float)]
 
 
+class hf_head_norm(ctypes.Structure):
+    _fields_ = [("eps", ctypes.c_float), ("per_head", ctypes.c_int32)]
+
+
+class hf_rope_scaling(ctypes.Structure):
+    _fields_ = [("factor", ctypes.c_double), ("trained", ctypes.c_double), ("slow", ctypes.c_double), ("fast", ctypes.c_double),
+                ("amplitude", ctypes.c_float), ("axes", ctypes.c_int32)]
+
+
 def _dtype(dtype):
     if isinstance(dtype, str):
         return {"bf16": HF_BF16, "f32": HF_F32}[dtype]
@@ -97,6 +106,17 @@ def make_paged(heads, heads_kv, head_dim, dtype, page_tokens, n_pages, n_seqs, m
                softmax_scale=0.0) -> hf_paged:
     return hf_paged(heads, heads_kv, head_dim, _dtype(dtype), page_tokens, n_pages, n_seqs, max_pages, int(causal), window, n_sink,
                     softmax_scale)
+
+
+def make_head_norm(eps=1e-6, per_head=False) -> hf_head_norm:
+    """per_head: the weights are [heads, head_dim], else [head_dim] for all heads."""
+    return hf_head_norm(eps, int(per_head))
+
+
+def make_rope_scaling(factor, trained, slow=1.0, fast=32.0, amplitude=1.0, axes=(0,)) -> hf_rope_scaling:
+    """Pairs of the given axes that make at most ``slow`` turns over the ``trained`` positions turn ``factor`` times slower, those with at
+    least ``fast`` turns as before, others in between; cosines and sines are multiplied by ``amplitude``."""
+    return hf_rope_scaling(factor, trained, slow, fast, amplitude, sum({1 << int(a) for a in axes}))
 
 
 def lib_path() -> str:
@@ -162,6 +182,13 @@ def load():
     lib.hf_paged_append.argtypes = [PP, AP, I, P, LP, P, LP, P, LP, P, P, P, P, P, P, P, LP, P]
     lib.hf_paged_workspace_bytes.argtypes = [PP, I, ctypes.POINTER(SZ)]
     lib.hf_paged_attn_fwd.argtypes = [PP, P, LP, I, P, P, P, P, P, P, LP, P, P, SZ, P]
+    NP, SP = ctypes.POINTER(hf_head_norm), ctypes.POINTER(hf_rope_scaling)
+    lib.hf_norm_rope_fwd.argtypes = [NP, AP, SP, I, I, I, I, I, P, LP, P, P, I, P, LP, P]
+    lib.hf_norm_rope_bwd_workspace_bytes.argtypes = [NP, I, I, I, I, ctypes.POINTER(SZ)]
+    lib.hf_norm_rope_bwd.argtypes = [NP, AP, SP, I, I, I, I, I, P, LP, P, P, I, P, LP, P, LP, P, P, SZ, P]
+    lib.hf_paged_append_e4m3.argtypes = [PP, NP, AP, SP, I, P, LP, P, LP, P, LP, P, P, P, P, P, P, P, P, P, P, P, LP, P]
+    lib.hf_paged_e4m3_workspace_bytes.argtypes = [PP, I, ctypes.POINTER(SZ)]
+    lib.hf_paged_attn_e4m3_fwd.argtypes = [PP, P, LP, I, P, P, P, P, P, P, P, P, LP, P, P, SZ, P]
     lib.hf_probe_mfma_bf16.argtypes = [I, P, ctypes.POINTER(ctypes.c_double), P]
     for name in ("hf_state_bytes", "hf_state_init", "hf_state_fold_linear", "hf_window_advance", "hf_absorb_evicted", "hf_absorb_workspace_bytes", "hf_select_k",
                  "hf_workspace_bytes",
@@ -172,14 +199,15 @@ def load():
                  "hf_state_planes", "hf_absorb_evicted_planes", "hf_hybrid_attn_fwd_planes", "hf_probe_mfma_bf16",
                  "hf_ring_open_chunk", "hf_ring_step", "hf_pooled_keys_bytes", "hf_pool_keys", "hf_select_attn_fwd",
                  "hf_step_workspace_bytes", "hf_step_fwd", "hf_rope_append_keys", "hf_ring_last_step", "hf_rope_axes_apply", "hf_paged_append",
-                 "hf_paged_workspace_bytes", "hf_paged_attn_fwd"):
+                 "hf_paged_workspace_bytes", "hf_paged_attn_fwd", "hf_norm_rope_fwd", "hf_norm_rope_bwd_workspace_bytes", "hf_norm_rope_bwd",
+                 "hf_paged_append_e4m3", "hf_paged_e4m3_workspace_bytes", "hf_paged_attn_e4m3_fwd"):
         getattr(lib, name).restype = ctypes.c_int
     try:
         from . import _marshal
     except ImportError as e:
         raise RuntimeError(f"the marshalling module does not load ({e}): build it with `python -m paper_2604_10103_amd.build`") from e
     _marshal.bind({name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _marshal.entry_names()}, HFError,
-                  hf_config, hf_window, hf_ring, hf_rope_axes, hf_paged)
+                  hf_config, hf_window, hf_ring, hf_rope_axes, hf_paged, hf_head_norm, hf_rope_scaling)
     _lib, _native = lib, _marshal
     return lib
 
@@ -469,3 +497,43 @@ def hf_paged_workspace_bytes(cache: hf_paged, n_q: int) -> int:
 def hf_paged_attn_fwd(cache: hf_paged, Q, cu_new, seq_lens, K_pages, V_pages, page_table, O, workspace=None, lse2=None) -> None:
     """Attention of every sequence's new tokens Q [rows, heads, head_dim] over its pages; lse2: optional fp32 [heads, rows] out."""
     _call().paged_attn_fwd(cache, Q, cu_new, seq_lens, K_pages, V_pages, page_table, O, workspace, lse2)
+
+
+def hf_norm_rope_fwd(X, Y, norm=None, weight=None, rope=None, positions=None, scaling=None) -> None:
+    """Y = the rows of X at unit mean square, weighted (fp32 [head_dim] or, norm.per_head, [heads, head_dim]; None: ones) and turned by
+    their tokens' positions; norm None: only turned, rope None: not turned.  X, Y: [batch, heads, tokens, head_dim] or packed [tokens,
+    heads, head_dim], strided views too (the last dimension contiguous, the other strides multiples of 16 bytes); Y may be X.
+    positions: int32 [axes, tokens] or [batch, axes, tokens]."""
+    _call().norm_rope_fwd(X, Y, norm, weight, rope, positions, scaling)
+
+
+def hf_norm_rope_bwd_workspace_bytes(norm: hf_head_norm, head_dim: int, batch: int, heads: int, n_tokens: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().hf_norm_rope_bwd_workspace_bytes(ctypes.byref(norm), head_dim, batch, heads, n_tokens, ctypes.byref(out)))
+    return out.value
+
+
+def hf_norm_rope_bwd(X, dY, dX, norm=None, weight=None, rope=None, positions=None, scaling=None, dweight=None, workspace=None) -> None:
+    """Gradients of hf_norm_rope_fwd: dX, and dweight (fp32, the weights' shape, with a workspace) if it is given; dX may be X or dY."""
+    _call().norm_rope_bwd(X, dY, dX, norm, weight, rope, positions, scaling, dweight, workspace)
+
+
+def hf_paged_append_e4m3(cache: hf_paged, K_new, V_new, cu_new, seq_lens, K_pages, V_pages, K_scales, V_scales, page_table, norm=None,
+                         k_weight=None, q_weight=None, rope=None, positions=None, scaling=None, Q=None, Q_out=None) -> None:
+    """hf_paged_append into pages in 8 bits: keys normalised (norm None: as they are) and turned (rope None: not), then keys and values
+    written as torch.float8_e4m3fn codes with an fp32 scale [n_pages, heads_kv, page_tokens] for each row; Q normalised and turned into
+    Q_out (may be Q).  k_weight, q_weight: as hf_norm_rope_fwd's weight."""
+    _call().paged_append_e4m3(cache, K_new, V_new, cu_new, seq_lens, K_pages, V_pages, K_scales, V_scales, page_table, norm, k_weight,
+                              q_weight, rope, positions, scaling, Q, Q_out)
+
+
+def hf_paged_e4m3_workspace_bytes(cache: hf_paged, n_q: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().hf_paged_e4m3_workspace_bytes(ctypes.byref(cache), n_q, ctypes.byref(out)))
+    return out.value
+
+
+def hf_paged_attn_e4m3_fwd(cache: hf_paged, Q, cu_new, seq_lens, K_pages, V_pages, K_scales, V_scales, page_table, O, workspace=None,
+                           lse2=None) -> None:
+    """hf_paged_attn_fwd over pages in 8 bits (torch.float8_e4m3fn codes, fp32 scales of their rows)."""
+    _call().paged_attn_e4m3_fwd(cache, Q, cu_new, seq_lens, K_pages, V_pages, K_scales, V_scales, page_table, O, workspace, lse2)

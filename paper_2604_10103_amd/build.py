@@ -36,6 +36,9 @@ SOURCES = [
     "hf_paged_attn.hip",
     "hf_paged_attn_f32.hip",
     "hf_api_paged.hip",
+    "hf_norm_rope.hip",
+    "hf_e4m3_attn.hip",
+    "hf_api_e4m3.hip",
     "hf_bwd.hip",
     "hf_bwd_mfma.hip",
     "hf_probe.hip",

@@ -25,7 +25,8 @@ namespace {
   X(hf_select_attn_fwd) X(hf_step_fwd) X(hf_hybrid_attn_fwd_save) X(hf_rope_window_indices) X(hf_rope_tables)               \
   X(hf_rope_append_keys) X(hf_rope_apply) X(hf_stream_open_chunk) X(hf_stream_step) X(hf_ring_open_chunk) X(hf_ring_step)   \
   X(hf_ring_last_step) X(hf_hybrid_attn_bwd) X(hf_hybrid_attn_bwd_saved) X(hf_rope_axes_apply) X(hf_paged_append)           \
-  X(hf_paged_attn_fwd) X(hf_paged_workspace_bytes)
+  X(hf_paged_attn_fwd) X(hf_paged_workspace_bytes) X(hf_norm_rope_fwd) X(hf_norm_rope_bwd) X(hf_paged_append_e4m3)            \
+  X(hf_paged_attn_e4m3_fwd)
 
 #define HF_POINTER(name) decltype(&::name) name = nullptr;
 struct {
@@ -81,6 +82,7 @@ const char* dtype_name(at::ScalarType t) {
     case at::kFloat: return "torch.float32";
     case at::kInt: return "torch.int32";
     case at::kByte: return "torch.uint8";
+    case at::kFloat8_e4m3fn: return "torch.float8_e4m3fn";
     default: return c10::toString(t);
   }
 }
@@ -632,7 +634,143 @@ PyObject* paged_attn_fwd(Args a) {   // cache, Q, cu_new, seq_lens, K_pages, V_p
   return none();
 }
 
-// bind(addresses by name, HFError, hf_config, hf_window, hf_ring, hf_rope_axes, hf_paged)
+// ---- norms with rotation, and the pages in 8 bits
+// rows [batch, heads, tokens, d], or packed [tokens, heads, d]: one batch, heads before tokens
+struct Rows {
+  at::ScalarType type;
+  int dims;
+  int64_t d;
+  Strided x;
+  Rows(PyObject* o, const char* name) {
+    const at::Tensor& t = tensor(o, name);
+    type = t.scalar_type() == at::kFloat ? at::kFloat : at::kBFloat16;
+    dims = (int)t.dim();
+    if (dims != 3 && dims != 4) raise(PyExc_ValueError, "%s must be [batch, heads, tokens, head_dim] or [tokens, heads, head_dim], got %d dimensions", name, dims);
+    d = t.size(dims - 1);
+    x = take(o, name);
+    for (int64_t v : {x.n[0], x.n[1], x.n[2], d})
+      if (v > INT32_MAX) raise(PyExc_OverflowError, "%lld does not fit in 32 bits", (long long)v);
+  }
+  Strided take(PyObject* o, const char* name) const {
+    Strided s = strided(o, name, type, dims - 1);
+    if (dims == 3 && o != Py_None) {
+      s.n[2] = s.n[0]; s.stride[2] = s.stride[0];
+      s.n[0] = 1; s.stride[0] = 0;
+    }
+    return s;
+  }
+  Strided like(PyObject* o, const char* name) const {
+    if (o == Py_None) return Strided();
+    const Strided s = strided(o, name, type, dims - 1);
+    same_shape(o, name, dims == 4 ? Shape{x.n[0], x.n[1], x.n[2], d} : Shape{x.n[2], x.n[1], d});
+    return take(o, name);
+  }
+  int dtype() const { return type == at::kFloat ? (int)HF_F32 : (int)HF_BF16; }
+  int batch() const { return (int)x.n[0]; }
+  int heads() const { return (int)x.n[1]; }
+  int tokens() const { return (int)x.n[2]; }
+};
+
+template <class T> struct Optional {   // a structure, or None
+  T value = {};
+  bool given;
+  Optional(PyObject* o, const char* name) : given(o != Py_None) {
+    if (given) value = *Struct<T>(o, name).get();
+  }
+  const T* get() const { return given ? &value : nullptr; }
+};
+
+// norm, rope, scaling and what goes with them
+struct NormRope {
+  const Optional<hf_head_norm> norm;
+  const Optional<hf_rope_axes> rope;
+  const Optional<hf_rope_scaling> scaling;
+  NormRope(PyObject* n, PyObject* r, PyObject* s) : norm(n, "hf_head_norm"), rope(r, "hf_rope_axes"), scaling(s, "hf_rope_scaling") {}
+  float* weight(PyObject* o, const char* name, int64_t heads, int64_t d) const {
+    return static_cast<float*>(norm.value.per_head ? here(o, name, at::kFloat, {heads, d}) : here(o, name, at::kFloat, {d}));
+  }
+};
+
+struct Positions {
+  const int32_t* p = nullptr;
+  int per_batch = 0;
+  Positions(PyObject* o, const NormRope& how, const Rows& r) {
+    if (o == Py_None) return;
+    if (!how.rope.given) raise(PyExc_ValueError, "positions without rope");
+    const int64_t axes = how.rope.value.n_axes;
+    per_batch = tensor(o, "positions").dim() == 3;
+    p = static_cast<const int32_t*>(per_batch ? here(o, "positions", at::kInt, {r.x.n[0], axes, r.x.n[2]}) : here(o, "positions", at::kInt, {axes, r.x.n[2]}));
+  }
+};
+
+PyObject* norm_rope_fwd(Args a) {   // X, Y, norm, weight, rope, positions, scaling
+  const Rows r(a[0], "X");
+  const Strided y = r.like(a[1], "Y");
+  const NormRope how(a[2], a[4], a[6]);
+  const float* w = how.weight(a[3], "weight", r.x.n[1], r.d);
+  const Positions pos(a[5], how, r);
+  call{lib.hf_norm_rope_fwd, how.norm.get(), how.rope.get(), how.scaling.get(), r.dtype(), (int)r.d, r.batch(), r.heads(), r.tokens(), r.x.p,
+       r.x.strides(), w, pos.p, pos.per_batch, y.p, y.strides(), stream()};
+  return none();
+}
+
+PyObject* norm_rope_bwd(Args a) {   // X, dY, dX, norm, weight, rope, positions, scaling, dweight, workspace
+  const Rows r(a[0], "X");
+  const Strided dy = r.like(a[1], "dY"), dx = r.like(a[2], "dX");
+  const NormRope how(a[3], a[5], a[7]);
+  const float* w = how.weight(a[4], "weight", r.x.n[1], r.d);
+  const Positions pos(a[6], how, r);
+  float* dw = how.weight(a[8], "dweight", r.x.n[1], r.d);
+  void* ws = bytes(a[9], "workspace");
+  if (a[9] != Py_None) on_current_device(THPVariable_Unpack(a[9]), "workspace");
+  call{lib.hf_norm_rope_bwd, how.norm.get(), how.rope.get(), how.scaling.get(), r.dtype(), (int)r.d, r.batch(), r.heads(), r.tokens(), r.x.p,
+       r.x.strides(), w, pos.p, pos.per_batch, dy.p, dy.strides(), dx.p, dx.strides(), dw, ws, size_of(a[9]), stream()};
+  return none();
+}
+
+struct Codes {   // pages in 8 bits: codes and scales
+  void* pages;
+  float* scales;
+  Codes(const Paged& c, PyObject* codes, const char* name, PyObject* s, const char* scales_name)
+      : pages(here(codes, name, at::kFloat8_e4m3fn, {c->n_pages, c->heads_kv, c->page_tokens, c->head_dim})),
+        scales(static_cast<float*>(here(s, scales_name, at::kFloat, {c->n_pages, c->heads_kv, c->page_tokens}))) {}
+};
+
+// cache, K_new, V_new, cu_new, seq_lens, K_pages, V_pages, K_scales, V_scales, page_table, norm, k_weight, q_weight, rope, positions, scaling, Q, Q_out
+PyObject* paged_append_e4m3(Args a) {
+  const Paged c(a[0]);
+  const int n = rows_of(a[1], "K_new");
+  const Strided k = c.rows(a[1], "K_new", n, c->heads_kv), v = c.rows(a[2], "V_new", n, c->heads_kv);
+  const int32_t *cu = c.ints(a[3], "cu_new", {c->n_seqs + 1}), *lens = c.ints(a[4], "seq_lens", {c->n_seqs});
+  const Codes kp(c, a[5], "K_pages", a[7], "K_scales"), vp(c, a[6], "V_pages", a[8], "V_scales");
+  const int32_t* table = c.ints(a[9], "page_table", {c->n_seqs, c->max_pages});
+  const NormRope how(a[10], a[13], a[15]);
+  const float *kw = how.weight(a[11], "k_weight", c->heads_kv, c->head_dim), *qw = how.weight(a[12], "q_weight", c->heads, c->head_dim);
+  if (a[14] != Py_None && !how.rope.given) raise(PyExc_ValueError, "positions without rope");
+  const int32_t* pos = c.ints(a[14], "positions", {how.rope.value.n_axes, n});
+  const Strided q = c.rows(a[16], "Q", n, c->heads), o = c.rows(a[17], "Q_out", n, c->heads);
+  call{lib.hf_paged_append_e4m3, c.get(), how.norm.get(), how.rope.get(), how.scaling.get(), n, k.p, k.strides(), v.p, v.strides(), q.p,
+       q.strides(), kw, qw, cu, lens, pos, kp.pages, vp.pages, kp.scales, vp.scales, table, o.p, o.strides(), stream()};
+  return none();
+}
+
+PyObject* paged_attn_e4m3_fwd(Args a) {   // cache, Q, cu_new, seq_lens, K_pages, V_pages, K_scales, V_scales, page_table, O, workspace, lse2
+  const Paged c(a[0]);
+  const int n = rows_of(a[1], "Q");
+  const Strided q = c.rows(a[1], "Q", n, c->heads);
+  const int32_t *cu = c.ints(a[2], "cu_new", {c->n_seqs + 1}), *lens = c.ints(a[3], "seq_lens", {c->n_seqs});
+  const Codes kp(c, a[4], "K_pages", a[6], "K_scales"), vp(c, a[5], "V_pages", a[7], "V_scales");
+  const int32_t* table = c.ints(a[8], "page_table", {c->n_seqs, c->max_pages});
+  const Strided o = c.rows(a[9], "O", n, c->heads);
+  void* ws = bytes(a[10], "workspace");
+  if (a[10] != Py_None) on_current_device(THPVariable_Unpack(a[10]), "workspace");
+  float* lse = static_cast<float*>(here(a[11], "lse2", at::kFloat, {c->heads, n}));
+  call{lib.hf_paged_attn_e4m3_fwd, c.get(), q.p, q.strides(), n, cu, lens, kp.pages, vp.pages, kp.scales, vp.scales, table, o.p, o.strides(),
+       lse, ws, size_of(a[10]), stream()};
+  return none();
+}
+
+// bind(addresses by name, HFError, hf_config, hf_window, hf_ring, hf_rope_axes, hf_paged, hf_head_norm, hf_rope_scaling)
 PyObject* bind(Args a) {
   if (!PyDict_Check(a[0])) raise(PyExc_TypeError, "bind takes a dict of addresses");
   auto address = [&](const char* name) -> void* {
@@ -654,6 +792,8 @@ PyObject* bind(Args a) {
   Class<hf_ring>::type = structure(a[4]);
   Class<hf_rope_axes>::type = structure(a[5]);
   Class<hf_paged>::type = structure(a[6]);
+  Class<hf_head_norm>::type = structure(a[7]);
+  Class<hf_rope_scaling>::type = structure(a[8]);
   Py_INCREF(a[1]);
   Py_XDECREF(error_class);
   error_class = a[1];
@@ -686,7 +826,7 @@ template <PyObject* (*F)(Args), int N> PyObject* method(PyObject*, PyObject* con
 
 #define HF_METHOD(name, n) {#name, (PyCFunction)(void*)(&method<name, n>), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
-    HF_METHOD(bind, 7), HF_METHOD(entry_names, 0), HF_METHOD(state_init, 2), HF_METHOD(state_fold_linear, 4),
+    HF_METHOD(bind, 9), HF_METHOD(entry_names, 0), HF_METHOD(state_init, 2), HF_METHOD(state_fold_linear, 4),
     HF_METHOD(state_planes, 3), HF_METHOD(absorb_evicted, 7), HF_METHOD(absorb_evicted_planes, 8), HF_METHOD(window_evict, 10),
     HF_METHOD(block_select, 8), HF_METHOD(block_select_static, 6), HF_METHOD(hybrid_attn_fwd, 12),
     HF_METHOD(hybrid_attn_fwd_planes, 12), HF_METHOD(hybrid_attn_fwd_save, 14), HF_METHOD(pool_keys, 5),
@@ -694,6 +834,7 @@ PyMethodDef methods[] = {
     HF_METHOD(rope_append_keys, 8), HF_METHOD(rope_apply, 5), HF_METHOD(stream_open_chunk, 9), HF_METHOD(stream_step, 13),
     HF_METHOD(ring_open_chunk, 8), HF_METHOD(ring_step, 13), HF_METHOD(ring_last_step, 17), HF_METHOD(hybrid_attn_bwd, 16),
     HF_METHOD(hybrid_attn_bwd_saved, 18), HF_METHOD(rope_axes_apply, 5), HF_METHOD(paged_append, 12), HF_METHOD(paged_attn_fwd, 10),
+    HF_METHOD(norm_rope_fwd, 7), HF_METHOD(norm_rope_bwd, 10), HF_METHOD(paged_append_e4m3, 18), HF_METHOD(paged_attn_e4m3_fwd, 12),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "argument marshalling of the hf library", -1, methods, nullptr, nullptr, nullptr, nullptr};

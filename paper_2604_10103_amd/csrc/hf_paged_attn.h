@@ -33,6 +33,23 @@
 namespace hf {
 
 constexpr int kKeyTile = 32;
+constexpr float kGrow = 8.0f;   // log2 units: a row's reference moves only when its maximum grew by more than 2^8
+
+// Tiles of bf16 in LDS: 16-byte unit u of key row r sits at u ^ swizzle(r) (conflict-free fragment reads)
+template <int D> __device__ __forceinline__ int k_swizzle(int r) {
+  return D == 128 ? (r & 15) : (((r >> 1) & 1) | (((r >> 2) ^ (r >> 3)) & 1) << 1 | (((r >> 3) ^ (r >> 4)) & 1) << 2);
+}
+template <int D> __device__ __forceinline__ int v_swizzle(int r) {
+  return D == 128 ? ((r & 3) << 2 | ((r >> 2) & 3)) : (((r >> 1) & 1) << 2 | ((r >> 2) & 3));
+}
+
+// n / d = n * magic >> shift (the result) for n < 2^31
+inline int magic_of(int d, uint32_t& magic) {
+  int bits = 0;
+  while ((1 << bits) < d) ++bits;
+  magic = (uint32_t)((1ull << (31 + bits)) / (unsigned)d + 1);
+  return 31 + bits;
+}
 
 struct PagedSchedule {
   int groups;                    // workgroups that may be parts of a row tile's work (32 rows: the grid, if there is work for so many)

@@ -37,17 +37,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 namespace {
 
-constexpr float kGrow = 8.0f;   // log2 units: a row's reference moves only when its maximum grew by more than 2^8
-
 __device__ uint4 zero_row[1];   // what keys that are none read as, where a lane has an address
-
-// 16-byte unit u of key row r sits at u ^ swizzle(r) (conflict-free fragment reads)
-template <int D> __device__ __forceinline__ int k_swizzle(int r) {
-  return D == 128 ? (r & 15) : (((r >> 1) & 1) | (((r >> 2) ^ (r >> 3)) & 1) << 1 | (((r >> 3) ^ (r >> 4)) & 1) << 2);
-}
-template <int D> __device__ __forceinline__ int v_swizzle(int r) {
-  return D == 128 ? ((r & 3) << 2 | ((r >> 2) & 3)) : (((r >> 1) & 1) << 2 | ((r >> 2) & 3));
-}
 
 template <int D, int NW, int KS> struct Shape {
   static constexpr int BM = 32 * NW, NT = 64 * NW * KS;
@@ -521,14 +511,6 @@ Plan plan_of(const hf_paged& c, int n_q) {
   p.grid = (int)((grid + 7) & ~7ll);
   p.sc.meets = key_tiles > 1;
   return p;
-}
-
-// n / d = n * magic >> shift (the result) for n < 2^31
-int magic_of(int d, uint32_t& magic) {
-  int bits = 0;
-  while ((1 << bits) < d) ++bits;
-  magic = (uint32_t)((1ull << (31 + bits)) / (unsigned)d + 1);
-  return 31 + bits;
 }
 
 // The counters' part of every workspace is as large, whatever the call: what a call of another shape left there are counters of its tag
