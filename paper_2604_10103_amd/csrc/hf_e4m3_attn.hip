@@ -93,13 +93,23 @@ struct PoolRows {
       : table(a.table + (long long)it.seq * a.max_pages), page_rows((uint32_t)a.heads_kv * (uint32_t)a.page),
         head_rows((uint32_t)it.head_kv * (uint32_t)a.page), ids(-1), ids_base(-kWave), key_last(it.held - 1),
         entry_last(it.held > 0 ? div_page(a, it.held - 1) : 0) {}
-  // of key start + at of the tile at `start`, lane by lane (start >= held: none)
-  __device__ __forceinline__ uint32_t row(const PagedAttnArgs& a, int start, int at, int lane) {
+  // of the keys of two tiles, at s0 and s1 (>= held: none), lane by lane
+  __device__ __forceinline__ uint32_t rows(const PagedAttnArgs& a, int s0, int s1, int lane) {
+    if (s1 == s0 + kKeyTile) return run<2 * kKeyTile>(a, s0, lane);   // (uniform)
+    const uint32_t r0 = run<kKeyTile>(a, s0, lane & 31), r1 = run<kKeyTile>(a, s1, lane & 31);
+    return lane < 32 ? r0 : r1;
+  }
+  __device__ __forceinline__ uint32_t row(const PagedAttnArgs& a, int start, int lane) { return run<kKeyTile>(a, start, lane & 31); }
+  // of N <= 64 keys from `start` on: of key start + at
+  template <int N> __device__ __forceinline__ uint32_t run(const PagedAttnArgs& a, int start, int at) {
     if (start > key_last) return 0;   // (uniform)
-    const int first = div_page(a, start), last = div_page(a, min(start + kKeyTile - 1, key_last));
+    const int first = div_page(a, start), last = div_page(a, min(start + N - 1, key_last));
     if (first < ids_base || last >= ids_base + kWave) {
+      const int lane = thread_id() & 63;
       ids_base = first;
       ids = first + lane <= entry_last ? table[first + lane] : -1;
+      // waited for here: where the paths join, the compiler would wait for these in every call, and so for all other requests
+      __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
     }
     const int key = min(start + at, key_last), entry = div_page(a, key), id = __shfl(ids, entry - ids_base, kWave);
     return is_page(a, id) ? (uint32_t)id * page_rows + head_rows + (uint32_t)(key - entry * a.page) : 0;
@@ -251,11 +261,11 @@ __global__ __launch_bounds__(64 * KS, sizeof(T) == 2 ? 2 : 1) void e4m3_few_kern
 #pragma unroll
       for (int pl = 0; pl < PL; ++pl) asm volatile("" : "+v"(qf[rb][s][pl]));
   if (count > 0) {
-    const uint32_t row0 = pool.row(a, start_of(0), lane & 31, lane), row1 = pool.row(a, start_of(1), lane & 31, lane);
+    const uint32_t row0 = pool.row(a, start_of(0), lane), row1 = pool.row(a, start_of(1), lane);
     request(row0, lds);
     request(row1, lds + SLOT);
   }
-  uint32_t row_next = count > 0 ? pool.row(a, start_of(2), lane & 31, lane) : 0;
+  uint32_t row_next = count > 0 ? pool.row(a, start_of(2), lane) : 0;
 
 #pragma unroll 1
   for (int i = 0; i < count; ++i) {
@@ -277,7 +287,7 @@ __global__ __launch_bounds__(64 * KS, sizeof(T) == 2 ? 2 : 1) void e4m3_few_kern
     const uint32_t rows = row_next;
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the slot has been read
     request(rows, lds + slot);
-    row_next = pool.row(a, start_of(i + 3), lane & 31, lane);
+    row_next = pool.row(a, start_of(i + 3), lane);
 
     // ---- S^T
     f32x4 s[RB][2];
@@ -413,25 +423,32 @@ __global__ __launch_bounds__(64 * KS, sizeof(T) == 2 ? 2 : 1) void e4m3_few_kern
   }
 }
 
+template <int D> __device__ __forceinline__ int v8_swizzle_32(int r) {   // where the lanes that are served together read 16 features of 8 keys each
+  return D == 128 ? ((r >> 1) & 1) << 1 | ((r >> 3) & 1) << 2 : ((r >> 3) & 1) << 1;
+}
+
 // ------------------------------------------------------------------------------------------------ chunks
 // NW wavefronts of 32 rows each share every tile of 32 keys.  Products are 32 x 32 x 16, as in the other paged kernel: lane (l32, h) holds
-// row l32's scores of the keys 8 j + 4 h + r.  A thread brings 16 or 8 codes of K and of V into registers three tiles ahead, and into LDS as
-// bf16 one tile ahead, with the scales beside them (a key's times c); one barrier a tile.
+// row l32's scores of the keys 8 j + 4 h + r.  K goes through registers and into LDS as bf16, two tiles ahead, with the scales beside it (a
+// key's times c); V goes there directly, as bytes, which every wavefront converts behind its transposing reads: of bf16 those would take
+// twice as long, 1070 of some 2000 cycles a tile.  One barrier a tile, behind the first product, whose fragments of K were read during the
+// previous tile's softmax.
 template <int D, int NW> struct ChunkShape {
   static constexpr int BM = 32 * NW, NT = 64 * NW;
-  static constexpr int ROWB = 2 * D, TILE = kKeyTile * ROWB, SLOT = 2 * TILE + 256;   // K, V, scales of both
+  static constexpr int ROWB = 2 * D, KT = kKeyTile * ROWB, VT = kKeyTile * D;    // a tile of K as bf16, of V as bytes
+  static constexpr int V = 6 * KT, SCALES = V + 6 * VT;                          // three slots of two tiles each; of scales, two
   static constexpr int OUT = BM * (D + 4) * 4 + BM * 8;
-  static constexpr int SPAN = 2 * SLOT > OUT ? 2 * SLOT : OUT;
+  static constexpr int SPAN = SCALES + 1024 > OUT ? SCALES + 1024 : OUT;
   static constexpr int LDS = SPAN + 16;
 };
 
 template <typename T, int D, int NW>
 __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void e4m3_chunk_kernel(const E4m3Launch args) {
   using S = ChunkShape<D, NW>;
-  constexpr int BM = S::BM, NT = S::NT, ROWB = S::ROWB, TILE = S::TILE, SLOT = S::SLOT, PL = sizeof(T) == 2 ? 1 : 3;
+  constexpr int BM = S::BM, NT = S::NT, ROWB = S::ROWB, KT = S::KT, VT = S::VT, PL = sizeof(T) == 2 ? 1 : 3;
   constexpr int NS = D / 16, ND = D / 32;                  // steps of S^T, 32-feature blocks of O^T
-  constexpr int TPR = NT / kKeyTile, CPT = D / TPR;        // threads of a key's row, and their codes
-  static_assert(CPT == 8 || CPT == 16, "one or two units of bf16");
+  constexpr int TPR = NT / (2 * kKeyTile), CPT = D / TPR;  // threads of a key's row, and their codes
+  static_assert(CPT == 16 || CPT == 32, "16 bytes, once or twice");
   extern __shared__ __attribute__((aligned(256))) char smem[];
 
   PagedItem it;
@@ -461,57 +478,63 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void e4m3_chunk_ke
   const FullTiles full(a, it, it.t0, row_view(a, it, div_group(a, min(it.first + 32 * wave, x_last))),
                        row_view(a, it, div_group(a, min(it.first + 32 * wave + 31, x_last))), bad_pages);
 
-  // ---- a tile's way into LDS: this thread's key, and its codes of it
+  // ---- the way of two tiles into LDS.  The wavefront knows their rows, a lane each
   PoolRows pool(a, it);
+  typedef __attribute__((address_space(3))) char* Lds;
+  const uint32_t lds = (uint32_t)(uintptr_t)(Lds)smem;
+  // K and the scales through registers: this thread's key, and its codes of it
   const int key_in = tid / TPR, part = tid % TPR;
   const uint8_t* const k_from = static_cast<const uint8_t*>(a.K_pages) + CPT * part;
-  const uint8_t* const v_from = static_cast<const uint8_t*>(a.V_pages) + CPT * part;
-  struct Staged {
-    uint32_t k[CPT / 4], v[CPT / 4];
-    float ks, vs;
+  struct Codes {
+    u32x4 w[CPT / 16];
   };
-  const auto fetch = [&](Staged& st, int i) {
-    const uint64_t row = pool.row(a, start_of(i), key_in, lane);
-    if constexpr (CPT == 16) {
-      const uint4 k = *reinterpret_cast<const uint4*>(k_from + row * D), v = *reinterpret_cast<const uint4*>(v_from + row * D);
-      st.k[0] = k.x; st.k[1] = k.y; st.k[2] = k.z; st.k[3] = k.w;
-      st.v[0] = v.x; st.v[1] = v.y; st.v[2] = v.z; st.v[3] = v.w;
-    } else {
-      const uint2 k = *reinterpret_cast<const uint2*>(k_from + row * D), v = *reinterpret_cast<const uint2*>(v_from + row * D);
-      st.k[0] = k.x; st.k[1] = k.y;
-      st.v[0] = v.x; st.v[1] = v.y;
-    }
-    st.ks = args.k_scales[row];
-    st.vs = args.v_scales[row];
-  };
-  const auto place = [&](const Staged& st, char* slot) {
+  const auto fetch_k = [&](uint32_t row) {
+    Codes c;
 #pragma unroll
-    for (int u = 0; u < CPT / 8; ++u) {
-      const int unit = CPT / 8 * part + u;
-      *reinterpret_cast<bf16x8*>(slot + key_in * ROWB + 16 * (unit ^ k_swizzle<D>(key_in))) = widen(st.k[2 * u], st.k[2 * u + 1]);
-      *reinterpret_cast<bf16x8*>(slot + TILE + key_in * ROWB + 16 * (unit ^ v_swizzle<D>(key_in))) = widen(st.v[2 * u], st.v[2 * u + 1]);
-    }
+    for (int u = 0; u < CPT / 16; ++u) c.w[u] = reinterpret_cast<const u32x4*>(k_from + (uint64_t)row * D)[u];
+    return c;
+  };
+  struct Scales {
+    float k, v;
+  };
+  const auto fetch_scales = [&](uint32_t row) { return Scales{args.k_scales[row], args.v_scales[row]}; };
+  const auto place_k = [&](const Codes& c, int slot) {
+    char* const to = smem + 2 * KT * slot + key_in * ROWB;   // (a tile's rows are those of the next one's)
+#pragma unroll
+    for (int u = 0; u < CPT / 8; ++u)
+      *reinterpret_cast<bf16x8*>(to + 16 * ((CPT / 8 * part + u) ^ k_swizzle<D>(key_in & 31))) = widen(c.w[u / 2][2 * (u & 1)], c.w[u / 2][2 * (u & 1) + 1]);
+  };
+  const auto place_scales = [&](const Scales& sc, int slot) {
+    float* const to = reinterpret_cast<float*>(smem + S::SCALES + 512 * slot) + key_in;
     if (part == 0) {
-      reinterpret_cast<float*>(slot + 2 * TILE)[key_in] = st.ks * a.c_scale;
-      reinterpret_cast<float*>(slot + 2 * TILE)[32 + key_in] = st.vs;
+      to[0] = sc.k * a.c_scale;
+      to[64] = sc.v;
+    }
+  };
+  // V as it is: 1 KB pieces, a wavefront's are NW apart
+  constexpr int RPP = 1024 / D, UPR = D / 16, NP = 2 * VT / 1024 / NW;   // keys of a piece, 16-byte units of a key, a wavefront's pieces
+  static_assert(NP == 1 || NP == 2, "pieces");
+  const uint64_t v_pool = reinterpret_cast<uint64_t>(a.V_pages);
+  struct VRows {
+    uint32_t r[NP];
+  };
+  const auto bring_v = [&](const VRows& rows, int slot) {
+#pragma unroll
+    for (int j = 0; j < NP; ++j) {
+      const int key = (RPP * (wave + NW * j) + lane / UPR) & 31;
+      const uint64_t from = v_pool + (uint64_t)rows.r[j] * D + 16 * ((lane % UPR) ^ v8_swizzle_32<D>(key));
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                   :: "s"(__builtin_amdgcn_readfirstlane(lds + S::V + 2 * VT * slot + 1024 * (wave + NW * j))), "v"(from) : "memory", "m0");
     }
   };
 
   // ---- LDS reads.  K fragment of step s: unit 2 s + h of row l32.  V^T fragment (feature 32 dt + l32; keys 16 t2 + 8 y + 4 h .. + 3) by
-  // transposing reads: a 16-lane group fetches 4 keys x 16 features in chunks of 8 bytes
-  typedef __attribute__((address_space(3))) char* Lds;
-  uint32_t k_addr[NS], v_addr[ND][2];
+  // transposing reads: a 16-lane group fetches 8 keys x 16 features in chunks of 8 bytes
+  uint32_t k_addr[NS];
 #pragma unroll
-  for (int s = 0; s < NS; ++s) k_addr[s] = l32 * ROWB + 16 * ((2 * s + h) ^ k_swizzle<D>(l32));
-  {
-    const int j16 = lane & 15, g16 = (lane >> 4) & 1, key = 4 * h + (j16 >> 2);
-#pragma unroll
-    for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-      for (int y = 0; y < 2; ++y)   // (the swizzles of rows 16 apart agree)
-        v_addr[dt][y] = (uint32_t)(uintptr_t)(Lds)smem + TILE + (key + 8 * y) * ROWB +
-                        16 * ((4 * dt + 2 * g16 + ((j16 & 3) >> 1)) ^ v_swizzle<D>(key + 8 * y)) + 8 * (j16 & 1);
-  }
+  for (int s = 0; s < NS; ++s) k_addr[s] = lds + l32 * ROWB + 16 * ((2 * s + h) ^ k_swizzle<D>(l32));
+  const int v_row = 4 * h + ((lane >> 1) & 3) + (lane & 8);   // (the swizzles of rows 16 apart agree)
+  const uint32_t v_at = lds + S::V + v_row * D + 16 * (((lane >> 4) & 1) ^ v8_swizzle_32<D>(v_row)) + 8 * (lane & 1);
 
   f32x16 o[ND];
 #pragma unroll
@@ -520,38 +543,59 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void e4m3_chunk_ke
     for (int r = 0; r < 16; ++r) o[dt][r] = 0.0f;
   float m_ref = -INFINITY, l_run = 0.0f;
   uint32_t seen = 0;
+
   bool odd = false;   // NaN codes lie next to rows that do not see them: they were left out (uniform)
 
-  // tile i, which lies in `slot`
-  const auto work = [&](int i, const int slot) {
+  bf16x8 kf[NS];
+  const auto read_k = [&](int slot) {
+#pragma unroll
+    for (int s = 0; s < NS; ++s) kf[s] = *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)(k_addr[s] + slot * KT);
+  };
+  Codes kc;    // on their way: in step p, K of the tiles of step p + 2, scales of p + 1 (and, into LDS, V of p + 1)
+  Scales sc;
+  uint32_t row_k = 0, row_s = 0;   // the thread's rows of what is requested next
+  VRows row_v = {};
+  uint32_t rows_next = 0;          // the wavefront's, of the step's tiles behind those
+  const auto k_row_of = [&](uint32_t rows) { return (uint32_t)__shfl((int)rows, key_in, kWave); };
+  const auto v_rows_of = [&](uint32_t rows) {
+    VRows v;
+#pragma unroll
+    for (int j = 0; j < NP; ++j) v.r[j] = (uint32_t)__shfl((int)rows, RPP * (wave + NW * j) + lane / UPR, kWave);
+    return v;
+  };
+
+  // tile i, the first or second (half) of the two in a slot, whose K fragments are in registers; behind the first one's product, everybody
+  // meets: K of the next slot and V of this one are there, and nobody is at the slot before any more
+  const auto tile = [&](int i, const int slot, const int half, const int par) __attribute__((always_inline)) {
     f32x16 sacc;
 #pragma unroll
     for (int r = 0; r < 16; ++r) sacc[r] = 0.0f;
+    if (active) {
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      const bf16x8 kf = *reinterpret_cast<const bf16x8*>(smem + slot + k_addr[s]);
+      for (int s = 0; s < NS; ++s)
 #pragma unroll
-      for (int pl = PL - 1; pl >= 0; --pl) sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[s][pl], sacc, 0, 0, 0);
+        for (int pl = PL - 1; pl >= 0; --pl) sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s], qf[s][pl], sacc, 0, 0, 0);
     }
-    auto v_frag = [&](int dt, int t2) {
-      const uint32_t at = slot + 16 * ROWB * t2;
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(uintptr_t)(v_addr[dt][0] + at));
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(uintptr_t)(v_addr[dt][1] + at));
-      const s16x8 both = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-      return __builtin_bit_cast(bf16x8, both);
-    };
-    bf16x8 vf[2][ND];
+    if (half == 0) __syncthreads();
+    if (!active) return;
+    // what the softmax needs first, then what the products need
+    const uint32_t scales = lds + S::SCALES + 512 * par + 128 * half + 16 * h;
+    const int v_off = VT * (2 * slot + half);
+    const auto four = [&](int j) { return *(const __attribute__((address_space(3))) f32x4*)(uintptr_t)(scales + 16 * j); };
+    f32x4 ks[4], vs[4];
 #pragma unroll
-    for (int t2 = 0; t2 < 2; ++t2)
+    for (int j = 0; j < 4; ++j) ks[j] = four(2 * j);
+    i32x2 vr[2][ND];
 #pragma unroll
-      for (int dt = 0; dt < ND; ++dt) vf[t2][dt] = v_frag(dt, t2);
-    const f32x4* const scales = reinterpret_cast<const f32x4*>(smem + slot + 2 * TILE) + h;
+    for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const f32x4 ks = scales[2 * j];
+      for (int t2 = 0; t2 < 2; ++t2)
+        vr[t2][dt] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((i32x2 __attribute__((address_space(3)))*)(uintptr_t)((v_at ^ (32 * dt)) + v_off + 16 * D * t2));
+    read_k(half == 0 ? 2 * slot + 1 : (2 * slot + 2) % 6);
+    __builtin_amdgcn_sched_barrier(0);
+    const float m_use = m_ref == -INFINITY ? 0.0f : m_ref;   // exponents against the row's reference, which rarely moves
 #pragma unroll
-      for (int r = 0; r < 4; ++r) sacc[4 * j + r] *= ks[r];
-    }
+    for (int r = 0; r < 16; ++r) sacc[r] = fmaf(sacc[r], ks[r >> 2][r & 3], -m_use);
     const bool all = full.has(i);
     uint32_t mine = 0;
     if (!all) {
@@ -566,33 +610,27 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void e4m3_chunk_ke
       seen |= sees;
 #pragma unroll
       for (int r = 0; r < 16; ++r) sacc[r] = masked_score(sacc[r], mine, 8 * (r >> 2) + (r & 3));
-      // a probability of zero does not make a NaN vanish: such values become zero here (no code is infinite)
-      auto nans = [](uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; };   // a half's top bit: its exponent is full
+      // a probability of zero does not make a NaN vanish: such codes become zero here
       uint32_t any = 0;
 #pragma unroll
-      for (int t2 = 0; t2 < 2; ++t2)
+      for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-        for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) any |= nans(__builtin_bit_cast(u32x4, vf[t2][dt])[e]);
+        for (int t2 = 0; t2 < 2; ++t2) any |= nan_codes((uint32_t)vr[t2][dt][0]) | nan_codes((uint32_t)vr[t2][dt][1]);
       if (__any(any != 0)) {
         odd = true;
 #pragma unroll
-        for (int t2 = 0; t2 < 2; ++t2)
+        for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-          for (int dt = 0; dt < ND; ++dt) {
-            u32x4 w = __builtin_bit_cast(u32x4, vf[t2][dt]);
+          for (int t2 = 0; t2 < 2; ++t2)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const uint32_t c = nans(w[e]);
-              w[e] &= ~(c | (c - (c >> 15)));
-            }
-            vf[t2][dt] = __builtin_bit_cast(bf16x8, w);
-          }
+            for (int e = 0; e < 2; ++e)
+              vr[t2][dt][e] = (int)((uint32_t)vr[t2][dt][e] & ~((nan_codes((uint32_t)vr[t2][dt][e]) >> 7) * 255u));
       }
     } else {
       seen = 1;
     }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) vs[j] = four(16 + 2 * j);
     // ---- online softmax in the exp2 domain (a row with a NaN keeps its reference: its sum is NaN in any case)
     float mx = max_of3(max_of3(max_of3(sacc[0], sacc[1], sacc[2]), max_of3(sacc[3], sacc[4], sacc[5]), max_of3(sacc[6], sacc[7], sacc[8])),
                        max_of3(sacc[9], sacc[10], sacc[11]), max_of3(sacc[12], sacc[13], max_of3(sacc[14], sacc[15], sacc[15])));
@@ -600,31 +638,28 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void e4m3_chunk_ke
       const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
       mx = max_of3(__uint_as_float(sw[0]), __uint_as_float(sw[1]), __uint_as_float(sw[1]));
     }
-    const bool grows = mx > m_ref + kGrow;
+    const bool grows = mx > (m_ref == -INFINITY ? -INFINITY : kGrow);
     if (__any(grows)) {
-      const float m_new = grows ? mx : m_ref;
+      const float more = grows ? mx : 0.0f, m_new = grows ? m_use + mx : m_ref;
       const float alpha = grows ? __builtin_amdgcn_exp2f(m_ref - m_new) : 1.0f;
       m_ref = m_new;
       l_run *= alpha;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sacc[r] -= more;
 #pragma unroll
       for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
     }
-    const float m_use = m_ref == -INFINITY ? 0.0f : m_ref;
     float psum = 0.0f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      sacc[r] = __builtin_amdgcn_exp2f(sacc[r] - m_use);
+      sacc[r] = __builtin_amdgcn_exp2f(sacc[r]);
       psum += sacc[r];
     }
     l_run += psum;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const f32x4 vs = scales[8 + 2 * j];
-#pragma unroll
-      for (int r = 0; r < 4; ++r) sacc[4 * j + r] *= vs[r];
-    }
+    for (int r = 0; r < 16; ++r) sacc[r] *= vs[r >> 2][r & 3];
     if (!all) {   // (a scale that is not finite)
 #pragma unroll
       for (int r = 0; r < 16; ++r) sacc[r] = __uint_as_float(and_mask(sacc[r], mine, 8 * (r >> 2) + (r & 3)));
@@ -641,31 +676,61 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void e4m3_chunk_ke
 #pragma unroll
     for (int t2 = 0; t2 < 2; ++t2)
 #pragma unroll
-      for (int dt = 0; dt < ND; ++dt)
+      for (int dt = 0; dt < ND; ++dt) {
+        const bf16x8 vf = widen((uint32_t)vr[t2][dt][0], (uint32_t)vr[t2][dt][1]);
 #pragma unroll
-        for (int pl = PL - 1; pl >= 0; --pl) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[t2][dt], pf[t2][pl], o[dt], 0, 0, 0);
+        for (int pl = PL - 1; pl >= 0; --pl) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[t2][pl], o[dt], 0, 0, 0);
+      }
+  };
+  // two tiles, and on the way of the next ones while the products run
+  const auto step = [&](int p, const int slot) __attribute__((always_inline)) {
+    const int par = p & 1;
+    tile(2 * p, slot, 0, par);
+    if (2 * p + 1 < count) tile(2 * p + 1, slot, 1, par);
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): what the last step has requested, V included
+    place_k(kc, (slot + 2) % 3);
+    place_scales(sc, par ^ 1);
+    bring_v(row_v, (slot + 2) % 3);
+    kc = fetch_k(row_k);
+    sc = fetch_scales(row_s);
+    row_s = row_k;
+    row_v = v_rows_of(rows_next);
+    rows_next = pool.rows(a, start_of(2 * p + 8), start_of(2 * p + 9), lane);
+    row_k = k_row_of(rows_next);
   };
 
-  // two sets of registers on their way: tiles i + 1 (placed in step i) and i + 2
-  Staged st[2];
   if (count > 0) {
-    fetch(st[0], 0);
-    fetch(st[1], 1);
-    place(st[0], smem);
-    fetch(st[0], 2);
+    const uint32_t r0 = pool.rows(a, start_of(0), start_of(1), lane), r1 = pool.rows(a, start_of(2), start_of(3), lane);
+    const uint32_t r2 = pool.rows(a, start_of(4), start_of(5), lane);
+    const Codes k0 = fetch_k(k_row_of(r0)), k1 = fetch_k(k_row_of(r1));
+    const Scales s0 = fetch_scales(k_row_of(r0));
+    bring_v(v_rows_of(r0), 0);
+    bring_v(v_rows_of(r1), 1);
+    row_s = k_row_of(r2);
+    kc = fetch_k(row_s);
+    sc = fetch_scales(k_row_of(r1));
+    row_v = v_rows_of(r2);
+    rows_next = pool.rows(a, start_of(6), start_of(7), lane);
+    row_k = k_row_of(rows_next);
+    place_k(k0, 0);
+    place_scales(s0, 0);
+    place_k(k1, 1);
   }
+  // nothing is on its way any more.  (Else the compiler would wait for the queries where the loop uses them, and so in every step for what that
+  // step has requested itself)
+  __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
+  __syncthreads();
+  if (count > 0) read_k(0);
 #pragma unroll 1
-  for (int i = 0; i < count; i += 2) {
-    __syncthreads();   // tile i is there, and everybody is done with tile i - 1
-    place(st[1], smem + SLOT);
-    fetch(st[1], i + 3);
-    if (active) work(i, 0);
-    if (i + 1 >= count) break;
-    __syncthreads();
-    place(st[0], smem);
-    fetch(st[0], i + 4);
-    if (active) work(i + 1, SLOT);
+  for (int p = 0; 2 * p < count; p += 3) {
+    step(p, 0);
+    if (2 * p + 2 >= count) break;
+    step(p + 1, 1);
+    if (2 * p + 4 >= count) break;
+    step(p + 2, 2);
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing may land on the sums
   __syncthreads();   // the sums lie over the tiles
 
   if (odd)
