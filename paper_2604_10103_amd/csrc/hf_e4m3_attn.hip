@@ -89,11 +89,25 @@ struct PoolRows {
   const int32_t* table;
   uint32_t page_rows, head_rows;
   int ids, ids_base, key_last, entry_last;
+  int two_at = -(1 << 30), two_inside = 0;
+  uint32_t two_rows = 0;
   __device__ __forceinline__ PoolRows(const PagedAttnArgs& a, const PagedItem& it)
       : table(a.table + (long long)it.seq * a.max_pages), page_rows((uint32_t)a.heads_kv * (uint32_t)a.page),
         head_rows((uint32_t)it.head_kv * (uint32_t)a.page), ids(-1), ids_base(-kWave), key_last(it.held - 1),
         entry_last(it.held > 0 ? div_page(a, it.held - 1) : 0) {}
-  // of the keys of two tiles, at s0 and s1 (>= held: none), lane by lane
+  // of the keys of two tiles, at s0 and s1 (>= held: none), lane by lane, where the last call's were 64 keys before: a page that holds both has
+  // its rows 64 further (of keys behind the sequence's the page's own, if there is one)
+  __device__ __forceinline__ uint32_t next_two(const PagedAttnArgs& a, int s0, int s1, int lane, bool bad_pages) {
+    const bool follows = s0 - 2 * kKeyTile == two_at && s1 == s0 + kKeyTile && s0 <= key_last && !bad_pages;   // (uniform)
+    two_at = s0;
+    if (follows && two_inside + 2 * kKeyTile + 63 < a.page) {   // (the first key's place; uniform)
+      two_inside += 2 * kKeyTile;
+      return two_rows += 2 * kKeyTile;
+    }
+    two_inside = s0 <= key_last ? s0 - div_page(a, s0) * a.page : a.page;
+    return two_rows = rows(a, s0, s1, lane);
+  }
+  // the same, found anew
   __device__ __forceinline__ uint32_t rows(const PagedAttnArgs& a, int s0, int s1, int lane) {
     if (s1 == s0 + kKeyTile) return run<2 * kKeyTile>(a, s0, lane);   // (uniform)
     const uint32_t r0 = run<kKeyTile>(a, s0, lane & 31), r1 = run<kKeyTile>(a, s1, lane & 31);
@@ -111,7 +125,14 @@ struct PoolRows {
       // waited for here: where the paths join, the compiler would wait for these in every call, and so for all other requests
       __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
     }
-    const int key = min(start + at, key_last), entry = div_page(a, key), id = __shfl(ids, entry - ids_base, kWave);
+    const int key = min(start + at, key_last), entry = div_page(a, key);
+    int id;
+    if (last <= first + 1) {   // two pages at most: no exchange through LDS, which would be waited for
+      const int id0 = __builtin_amdgcn_readlane(ids, first - ids_base), id1 = __builtin_amdgcn_readlane(ids, last - ids_base);
+      id = entry == first ? id0 : id1;
+    } else {
+      id = __shfl(ids, entry - ids_base, kWave);
+    }
     return is_page(a, id) ? (uint32_t)id * page_rows + head_rows + (uint32_t)(key - entry * a.page) : 0;
   }
 };
@@ -551,7 +572,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void e4m3_chunk_ke
 #pragma unroll
     for (int s = 0; s < NS; ++s) kf[s] = *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)(k_addr[s] + slot * KT);
   };
-  Codes kc;    // on their way: in step p, K of the tiles of step p + 2, scales of p + 1 (and, into LDS, V of p + 1)
+  Codes kc;    // on their way: when step p begins, K of the tiles of step p + 1, their scales' and V's of p (V into LDS)
   Scales sc;
   uint32_t row_k = 0, row_s = 0;   // the thread's rows of what is requested next
   VRows row_v = {};
@@ -564,9 +585,24 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void e4m3_chunk_ke
     return v;
   };
 
-  // tile i, the first or second (half) of the two in a slot, whose K fragments are in registers; behind the first one's product, everybody
-  // meets: K of the next slot and V of this one are there, and nobody is at the slot before any more
-  const auto tile = [&](int i, const int slot, const int half, const int par) __attribute__((always_inline)) {
+  // step p's share of this, into `slot`
+  const auto on_the_way = [&](int p, const int slot) __attribute__((always_inline)) {
+    __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): what the last step has requested, V included
+    place_k(kc, slot);
+    place_scales(sc, p & 1);
+    bring_v(row_v, slot);
+    kc = fetch_k(row_k);
+    sc = fetch_scales(row_s);
+    row_s = row_k;
+    row_v = v_rows_of(rows_next);
+    rows_next = pool.next_two(a, start_of(2 * p + 6), start_of(2 * p + 7), lane, bad_pages);
+    row_k = k_row_of(rows_next);
+  };
+
+  // tile i, the first or second (half) of the two in a slot, whose K fragments are in registers.  Behind the first one's product, and the next
+  // tiles' way while it runs, everybody meets: K of the next slot and V of this one are there, and nobody is at the slot before any more
+  const auto tile = [&](int i, const int slot, const int half) __attribute__((always_inline)) {
+    const int par = (i / 2) & 1;
     f32x16 sacc;
 #pragma unroll
     for (int r = 0; r < 16; ++r) sacc[r] = 0.0f;
@@ -576,7 +612,11 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void e4m3_chunk_ke
 #pragma unroll
         for (int pl = PL - 1; pl >= 0; --pl) sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s], qf[s][pl], sacc, 0, 0, 0);
     }
-    if (half == 0) __syncthreads();
+    if (half == 0) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (i > 0) on_the_way(i / 2, (slot + 1) % 3);
+      __syncthreads();
+    }
     if (!active) return;
     // what the softmax needs first, then what the products need
     const uint32_t scales = lds + S::SCALES + 512 * par + 128 * half + 16 * h;
@@ -682,22 +722,9 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void e4m3_chunk_ke
         for (int pl = PL - 1; pl >= 0; --pl) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[t2][pl], o[dt], 0, 0, 0);
       }
   };
-  // two tiles, and on the way of the next ones while the products run
   const auto step = [&](int p, const int slot) __attribute__((always_inline)) {
-    const int par = p & 1;
-    tile(2 * p, slot, 0, par);
-    if (2 * p + 1 < count) tile(2 * p + 1, slot, 1, par);
-    __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): what the last step has requested, V included
-    place_k(kc, (slot + 2) % 3);
-    place_scales(sc, par ^ 1);
-    bring_v(row_v, (slot + 2) % 3);
-    kc = fetch_k(row_k);
-    sc = fetch_scales(row_s);
-    row_s = row_k;
-    row_v = v_rows_of(rows_next);
-    rows_next = pool.rows(a, start_of(2 * p + 8), start_of(2 * p + 9), lane);
-    row_k = k_row_of(rows_next);
+    tile(2 * p, slot, 0);
+    if (2 * p + 1 < count) tile(2 * p + 1, slot, 1);
   };
 
   if (count > 0) {
@@ -711,7 +738,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void e4m3_chunk_ke
     kc = fetch_k(row_s);
     sc = fetch_scales(k_row_of(r1));
     row_v = v_rows_of(r2);
-    rows_next = pool.rows(a, start_of(6), start_of(7), lane);
+    rows_next = pool.next_two(a, start_of(6), start_of(7), lane, bad_pages);
     row_k = k_row_of(rows_next);
     place_k(k0, 0);
     place_scales(s0, 0);
