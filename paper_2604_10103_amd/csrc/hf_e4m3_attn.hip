@@ -812,13 +812,25 @@ Plan plan_of(const hf_paged& c, int n_q) {
   }
   p.ks = p.rows <= 32 ? 4 : 1;
   const bool wide = c.head_dim == 128;
+  const long long key_tiles = ((long long)c.max_pages * c.page_tokens + kKeyTile - 1) / kKeyTile;   // (at most)
   if (p.rows <= 32) {
-    if (tiles(p.rows) >= 2048) {   // a row tile a wavefront
+    // Eight wavefronts share a row tile's keys, one workgroup a compute unit, where there are few row tiles or their keys may be many: half as
+    // many parts of a row meet (four tokens over 131071 keys 65 us, with four wavefronts and two workgroups a unit 84; 64 single tokens over 410 to
+    // 8191 117 and 134).  More row tiles of shorter sequences find two to four chains on their unit, each of which waits for its own: 64 single
+    // tokens over 1025 keys 28 us by four wavefronts, 34 by eight; 200 over 100 to 2000 105 and 119; and, where there is one for all 2048
+    // wavefronts, a row tile a wavefront.
+    if (tiles(p.rows) >= 2048) {
       p.ks = 1;
       p.sc.groups = 2048;
       p.sc.tile = wide ? 3.2f : 1.6f;
       p.sc.tile_alone = wide ? 1.2f : 0.9f;
       p.sc.lead = 2;
+    } else if (p.rows == 16 ? tiles(16) <= 400 || key_tiles >= 192 : c.dtype == HF_BF16 && tiles(32) <= 64) {
+      p.ks = 8;
+      p.sc.groups = 256;
+      p.sc.tile = wide ? 0.4f : 0.2f;
+      p.sc.tile_alone = wide ? 0.3f : 0.2f;
+      p.sc.lead = 10;
     } else {
       p.sc.groups = 512;
       p.sc.tile = wide ? 0.8f : 0.4f;
@@ -847,7 +859,6 @@ Plan plan_of(const hf_paged& c, int n_q) {
       p.sc.tile_alone = wide ? 0.7f : 0.4f;
     }
   }
-  const long long key_tiles = ((long long)c.max_pages * c.page_tokens + kKeyTile - 1) / kKeyTile;   // (at most)
   long long grid = p.rows <= 32 ? p.sc.groups : tiles(p.rows) + p.sc.groups;
   if (grid > tiles(p.rows) * key_tiles) grid = tiles(p.rows) * key_tiles;
   p.grid = (int)((grid + 7) & ~7ll);
@@ -872,9 +883,13 @@ template <typename T, int D> int launch_of(const E4m3Launch& l, const Plan& p, h
   }
   if (p.rows == 128) return launch<e4m3_chunk_kernel<T, D, 4>, ChunkShape<D, 4>>(l, p.grid, s);
   if (p.rows == 32) {
+    if constexpr (sizeof(T) == 2) {   // (fp32: more registers than eight wavefronts have)
+      if (p.ks == 8) return launch<e4m3_few_kernel<T, D, 2, 8>, FewShape<D, 2, 8>>(l, p.grid, s);
+    }
     if (p.ks == 1) return launch<e4m3_few_kernel<T, D, 2, 1>, FewShape<D, 2, 1>>(l, p.grid, s);
     return launch<e4m3_few_kernel<T, D, 2, 4>, FewShape<D, 2, 4>>(l, p.grid, s);
   }
+  if (p.ks == 8) return launch<e4m3_few_kernel<T, D, 1, 8>, FewShape<D, 1, 8>>(l, p.grid, s);
   if (p.ks == 1) return launch<e4m3_few_kernel<T, D, 1, 1>, FewShape<D, 1, 1>>(l, p.grid, s);
   return launch<e4m3_few_kernel<T, D, 1, 4>, FewShape<D, 1, 4>>(l, p.grid, s);
 }
