@@ -3,7 +3,7 @@
 //
 // All move every row once: they are bound by memory.  A thread owns the same 8 or 16 features of a token for several heads, so that an angle
 // is formed once and serves them all; a row's 4 to 16 threads exchange their sums of squares (and the gradient's products, and the largest
-// magnitude of a row that is quantised) by data-parallel moves within 16 lanes, three or four instructions a sum.  Four rows are requested
+// magnitude of a row that is quantised) by data-parallel moves within 16 lanes, three or four instructions a sum.  Two rows are requested
 // before the first one is worked on.
 #include <math.h>
 
@@ -151,7 +151,7 @@ template <typename T, int D, int MODE, class From, class Weight, class Out>
 __device__ __forceinline__ void norm_rows(const NormArgs& n, const Angles<D, MODE>& t, int g, int P, int i0, int i1, bool shared, From from, Weight weight,
                                           Out out) {
   typedef Part<T, D, MODE> R;
-  constexpr int U = 4, NF = R::NF;
+  constexpr int NF = R::NF, U = 2;
   if (i0 >= i1) return;
   float w[NF];
   if (shared) R::weights(weight(0), g, P, w);
@@ -237,7 +237,7 @@ struct BwdArgs {
 template <typename T, int D, int MODE>
 __global__ __launch_bounds__(256) void norm_rope_bwd_kernel(const AxesSpec spec, const BwdArgs a) {
   typedef Part<T, D, MODE> R;
-  constexpr int TPT = R::TPR, TOK = 256 / TPT, NF = R::NF, U = 2;
+  constexpr int TPT = R::TPR, TOK = 256 / TPT, NF = R::NF, U = 1;
   const int g = threadIdx.x % TPT, P = spec.pairs;
   const int per = (a.heads + gridDim.y - 1) / gridDim.y, h0 = blockIdx.y * per, h1 = min(a.heads, h0 + per);
   const bool shared = !a.norm.per_head || !a.weight;
@@ -247,19 +247,23 @@ __global__ __launch_bounds__(256) void norm_rope_bwd_kernel(const AxesSpec spec,
   if (shared) R::weights(a.weight, g, P, w);
   for (int tok = blockIdx.x * TOK + threadIdx.x / TPT; tok < a.n; tok += gridDim.x * TOK) {
     const int32_t* pos = a.positions + blockIdx.z * a.pos_batch + tok;
-    Angles<D, MODE> t;
-    form_angles(t, spec, g, true, a.norm.amplitude, [&](int ax) { return pos[(long long)ax * a.n]; });
     const T* x = static_cast<const T*>(a.X) + blockIdx.z * a.xb + tok * a.xt;
     const T* dy = static_cast<const T*>(a.dY) + blockIdx.z * a.gb + tok * a.gt;
     T* dx = static_cast<T*>(a.dX) + blockIdx.z * a.db + tok * a.dt;
-    for (int h = h0; h < h1; h += U) {
-      typename R::Raw rx[U], rg[U];
+    typename R::Raw rx[U], rg[U];
+    const auto request = [&](int h) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int hu = min(h + u, h1 - 1);
         rx[u] = R::load(x + hu * a.xh, g, P);
         rg[u] = R::load(dy + hu * a.gh, g, P);
       }
+    };
+    request(h0);   // (on their way while the angles are formed)
+    Angles<D, MODE> t;
+    form_angles(t, spec, g, true, a.norm.amplitude, [&](int ax) { return pos[(long long)ax * a.n]; });
+    for (int h = h0; h < h1; h += U) {
+      if (h > h0) request(h);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         if (h + u >= h1) break;
@@ -449,10 +453,11 @@ __global__ __launch_bounds__(256) void append_e4m3_kernel(const AxesSpec spec, c
       [&](int h) { return weight_of(a.q_weight, h); }, [&](int h, const float (&x)[NF]) { R::store(o + h * a.oh, g, spec.pairs, x); });
 }
 
-// shares of a token's rows, as many workgroups as they fill the chip with: 2048 where that leaves each four rows, else 1024
-int shares(long long groups, int rows) {
-  const auto for_groups = [&](int n) { return (n + groups - 1) / groups; };
-  long long s = std::min(for_groups(2048), std::max(for_groups(1024), (long long)rows / 4));
+// shares of a token's rows: at least 1024 workgroups, or as many as leave each four rows, which an angle formed once serves; but no more than
+// the `resident` ones that run at a time, whose registers let the compute units have so many: 10800 tokens of 40 rows 47.2 us by 2025
+// workgroups, 48.5 by 2700; 9360 tokens of 36 rows into the pages 30.2 by 1170, 34.7 by 2340
+int shares(long long groups, int rows, int resident) {
+  const long long s = std::min(std::max(1ll, resident / groups), std::max((1024 + groups - 1) / groups, (long long)rows / 4));
   return (int)std::max(1ll, std::min(s, (long long)rows));
 }
 
@@ -488,9 +493,10 @@ BwdGrid bwd_grid(int D, int threads, int batch, int heads, int n, bool per_head)
   b.rows = per_head ? heads : 1;
   if (n == 0) return b;   // (no sums: zeros)
   const long long blocks = (n + tok - 1) / tok;
-  b.y = per_head ? heads : (int)std::max(1ll, std::min<long long>(shares(blocks * batch, heads), heads));
+  b.y = per_head ? heads : (int)std::max(1ll, std::min<long long>(shares(blocks * batch, heads, 2048), heads));
   const long long most = std::max(1ll, 1024ll / std::min<long long>((long long)b.y * b.z, 1024));
-  b.x = (int)std::max(1ll, std::min(blocks, most));
+  const long long turns = (blocks + most - 1) / most;   // all workgroups take as many blocks of tokens, or one less
+  b.x = (int)std::max(1ll, (blocks + turns - 1) / turns);
   b.parts = b.x * b.z * (per_head ? 1 : b.y);
   return b;
 }
@@ -520,7 +526,7 @@ int launch_norm_rope(const hf_head_norm* norm, const hf_rope_axes* r, const hf_r
                      norm_args(norm, sc)};
   const AxesMode mode = r ? axes_mode(*r, spec.pairs) : kAdjacent;
   const int tok = mode == kAdjacent ? 2048 / D : 4096 / D, groups = (n + tok - 1) / tok;
-  const dim3 grid(groups, shares((long long)groups * batch, heads), batch);
+  const dim3 grid(groups, shares((long long)groups * batch, heads, 2048), batch);
 #define HF_GO(T, DD, M) hipLaunchKernelGGL((norm_rope_kernel<T, DD, M>), grid, dim3(256), 0, s, spec, a)
   HF_ROPE_TYPES(dtype, D, mode, HF_GO);
 #undef HF_GO
@@ -568,7 +574,7 @@ int launch_append_e4m3(const hf_paged& c, const hf_head_norm* norm, const hf_rop
                         n, c.heads, c.heads_kv, c.page_tokens, c.n_pages, c.n_seqs, c.max_pages, norm_args(norm, sc)};
   const AxesMode mode = r ? axes_mode(*r, spec.pairs) : kAdjacent;
   const int D = c.head_dim, tok = mode == kAdjacent ? 2048 / D : 4096 / D, groups = (n + tok - 1) / tok;
-  const dim3 grid(groups, shares(groups, 2 * c.heads_kv + (Q ? c.heads : 0)));
+  const dim3 grid(groups, shares(groups, 2 * c.heads_kv + (Q ? c.heads : 0), 1536));
 #define HF_GO(T, DD, M) hipLaunchKernelGGL((append_e4m3_kernel<T, DD, M>), grid, dim3(256), 0, s, spec, a)
   HF_ROPE_TYPES(c.dtype, D, mode, HF_GO);
 #undef HF_GO
