@@ -729,6 +729,7 @@ HF_API int hf_paged_attn_fwd(const hf_paged* cache, const void* Q, const int64_t
  *   norm      NULL: none; its per_head holds for both weights.  k_weight, q_weight: as hf_norm_rope_fwd's, NULL: ones
  *   rope, scaling, positions, K_new, V_new, Q, Q_out, n_new   as for hf_paged_append and hf_norm_rope_fwd; values are only quantised.
  *             Neither norm nor rope: keys are only quantised, queries copied
+ * Two tokens of one call that name the same slot leave either of them there, or parts of both (codes of one, the scale of the other).
  * What is written (pages, scales, Q_out) lies over nothing else that the call is given. */
 HF_API int hf_paged_append_e4m3(const hf_paged* cache, const hf_head_norm* norm_or_null, const hf_rope_axes* rope_or_null,
                   const hf_rope_scaling* scaling_or_null, int32_t n_new, const void* K_new, const int64_t* k_strides, const void* V_new,
@@ -744,7 +745,7 @@ HF_API int hf_paged_e4m3_workspace_bytes(const hf_paged* cache, int32_t n_q, siz
  * key's scale with its score and a value's with its probability, so that nothing of the cache is rounded again: fp32 scores, statistics
  * and sums; in bf16 the product of probability and scale is rounded to bf16 for the second product.  What a token does not see, it does
  * not depend on, codes and scales that are NaN or infinite included; a NaN that it sees (code or scale) makes the outputs that it enters
- * NaN. */
+ * NaN.  (Scales are meant as hf_paged_append_e4m3 writes them: what an infinite one that is seen gives is not defined.) */
 HF_API int hf_paged_attn_e4m3_fwd(const hf_paged* cache, const void* Q, const int64_t* q_strides, int32_t n_q,
                   const int32_t* cu_new, const int32_t* seq_lens, const void* K_pages, const void* V_pages, const float* K_scales,
                   const float* V_scales, const int32_t* page_table, void* O, const int64_t* o_strides, float* lse2_or_null,
