@@ -638,7 +638,7 @@ HF_API int hf_norm_rope_bwd_workspace_bytes(const hf_head_norm* norm, int32_t he
  *   X, dY, dX  [batch, heads, n_tokens, head_dim], strides as above; strides of X and dY may be zero (one row for many), where dX still
  *              gets the gradient of every place.  dX may be X or dY (the same address and strides), otherwise it overlaps neither
  *   dweight_or_null  out fp32, the shape of the weights (also where `weight` is NULL: ones); norm given.  Written whole, zeros if there are
- *              no tokens.  The sum is formed in fp32 in a fixed order: the same bits every time
+ *              no tokens.  The sum is formed in a fixed order: the same bits every time
  *   workspace  for dweight: >= hf_norm_rope_bwd_workspace_bytes bytes, 256-byte aligned, no initialisation needed; NULL without dweight.
  *              Two calls that may overlap in time must not share one */
 HF_API int hf_norm_rope_bwd(const hf_head_norm* norm_or_null, const hf_rope_axes* rope_or_null, const hf_rope_scaling* scaling_or_null,

@@ -223,7 +223,7 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(const AxesSpec spec, con
 // ---- gradients.  With g the output's gradient turned back and u the row at unit mean square,
 //     dX = r (w g - u mean(w g u)),  dweight = sum g u:
 // one pass over X and dY.  Every thread sums its features of dweight over all its rows, in fp32; a workgroup's threads meet in LDS, and the
-// workgroups' sums lie in the workspace until a second launch adds them, in a fixed order
+// workgroups' sums lie in the workspace until a second launch adds them, in a fixed order, both in 64 bits
 struct BwdArgs {
   const void *X, *dY;
   void* dX;
@@ -298,9 +298,10 @@ __global__ __launch_bounds__(256) void norm_rope_bwd_kernel(const AxesSpec spec,
   for (int e = 0; e < NF; ++e) sums[threadIdx.x / TPT][R::feature(g, P, e)] = dw[e];
   __syncthreads();
   if (threadIdx.x < D) {
-    float s = 0.0f;
+    double total = 0.0;   // (of either sign: sums in 32 bits would cost half a digit)
 #pragma unroll
-    for (int i = 0; i < TOK; ++i) s += sums[i][threadIdx.x];
+    for (int i = 0; i < TOK; ++i) total += (double)sums[i][threadIdx.x];
+    const float s = (float)total;
     const int row = a.norm.per_head ? blockIdx.y : 0, shares = a.norm.per_head ? 1 : gridDim.y, share = a.norm.per_head ? 0 : blockIdx.y;
     const int parts = gridDim.x * gridDim.z * shares, part = (blockIdx.z * shares + share) * gridDim.x + blockIdx.x;
     a.partial[((long long)row * parts + part) * D + threadIdx.x] = s;
@@ -311,17 +312,17 @@ __global__ __launch_bounds__(256) void norm_rope_bwd_kernel(const AxesSpec spec,
 __global__ __launch_bounds__(1024) void norm_dweight_kernel(const float* partial, float* dweight, int parts, int D) {
   const int f = blockIdx.x * 32 + (threadIdx.x & 31), lane = threadIdx.x >> 5;
   const float* p = partial + (long long)blockIdx.y * parts * D + f;
-  float s = 0.0f;
+  double s = 0.0;
 #pragma unroll 8
-  for (int i = lane; i < parts; i += 32) s += p[(long long)i * D];
-  __shared__ float sums[32][33];
+  for (int i = lane; i < parts; i += 32) s += (double)p[(long long)i * D];
+  __shared__ double sums[32][33];
   sums[lane][threadIdx.x & 31] = s;
   __syncthreads();
   if (lane == 0) {
-    s = 0.0f;
+    s = 0.0;
 #pragma unroll
     for (int i = 0; i < 32; ++i) s += sums[i][threadIdx.x];
-    dweight[(long long)blockIdx.y * D + f] = s;
+    dweight[(long long)blockIdx.y * D + f] = (float)s;
   }
 }
 
