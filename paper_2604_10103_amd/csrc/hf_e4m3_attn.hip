@@ -196,7 +196,7 @@ __global__ __launch_bounds__(64 * KS, sizeof(T) == 2 ? 2 : 1) void e4m3_few_kern
   PagedCursor cursor;
   {
     const PagedLaunch p = launch_arguments();
-    cursor = first_item<BM, true>(p.a, p.sc);
+    cursor = first_item<BM, true, true>(p.a, p.sc);
   }
   for (bool again = false;; again = true) {
   PagedItem it;
@@ -824,16 +824,16 @@ Plan plan_of(const hf_paged& c, int n_q) {
   if (p.rows <= 32) {
     // Eight wavefronts share a row tile's keys, one workgroup a compute unit, where there are few row tiles or their keys may be many: half as
     // many parts of a row meet (four tokens over 131071 keys 65 us, with four wavefronts and two workgroups a unit 84; 64 single tokens over 410 to
-    // 8191 117 and 134).  More row tiles of shorter sequences find two to four chains on their unit, each of which waits for its own: 64 single
-    // tokens over 1025 keys 28 us by four wavefronts, 34 by eight; 200 over 100 to 2000 105 and 119; and, where there is one for all 2048
-    // wavefronts, a row tile a wavefront.
+    // 8191 117 and 134; 8 over 800 to 16000 36 and 42; eight tokens over 60000 44 and 65).  More row tiles of shorter sequences find two to four
+    // chains on their unit, each of which waits for its own: 64 single tokens over 1025 keys 34 us by eight wavefronts, 28 by four; 200 over 100 to
+    // 2000 119 and 105; and, where there is one for all 2048 wavefronts, a row tile a wavefront.
     if (tiles(p.rows) >= 2048) {
       p.ks = 1;
       p.sc.groups = 2048;
       p.sc.tile = wide ? 3.2f : 1.6f;
       p.sc.tile_alone = wide ? 1.2f : 0.9f;
       p.sc.lead = 2;
-    } else if (p.rows == 16 ? tiles(16) <= 400 || key_tiles >= 192 : c.dtype == HF_BF16 && tiles(32) <= 64) {
+    } else if ((c.dtype == HF_BF16 || p.rows == 16) && (tiles(p.rows) <= 400 || key_tiles >= 112)) {
       p.ks = 8;
       p.sc.groups = 256;
       p.sc.tile = wide ? 0.4f : 0.2f;

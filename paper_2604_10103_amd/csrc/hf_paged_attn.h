@@ -249,7 +249,7 @@ template <int BM> __device__ __forceinline__ void find_extent(const PagedAttnArg
   block.split = !p.shares && layers(block.q, p.C) > 1 ? block.extent : 0;
 }
 
-template <int BM, bool kShares> __device__ __forceinline__ PagedWork find_work(const PagedAttnArgs& a, const PagedSchedule& sc, SeqBlock& block) {
+template <int BM, bool kShares, bool kRagged = false> __device__ __forceinline__ PagedWork find_work(const PagedAttnArgs& a, const PagedSchedule& sc, SeqBlock& block) {
   const int lane = thread_id() & 63;
   const auto add = [](float x, float y) { return x + y; };
   const auto larger = [](float x, float y) { return fmaxf(x, y); };
@@ -274,12 +274,14 @@ template <int BM, bool kShares> __device__ __forceinline__ PagedWork find_work(c
     const float S = lane < 32 ? (float)(lane + 1) : floorf(32.0f * __builtin_amdgcn_exp2f((float)(lane - 31) * (5.0f / 32.0f)));   // .. 1024
     const float x = n * S * (1.0f / sc.units), full = fminf(x, 1.0f);
     const bool alike = units > 0.98f * longest * rows || (!kShares && lane > 0);
-    const bool once = kShares ? x <= 1.0f && rows * heads <= sc.units : x <= 1.0f;   // (those that stay have theirs from the beginning)
+    // (kRagged: row tiles of different lengths have half a piece more each than n S, and more than there are units would be another round)
+    const float pieces = kRagged && !alike && lane > 0 ? n * S + 0.5f * rows * heads : n * S;
+    const bool once = kShares ? (kRagged ? pieces <= sc.units : x <= 1.0f) && rows * heads <= sc.units : x <= 1.0f;   // (those that stay have theirs from the beginning)
     const float rounds = once ? 1.0f : (alike ? ceilf(x) : x + (kShares ? 0.75f : 0.5f));
     const float work = kShares ? rounds * fmaxf(sc.tile_alone + 0.3f * sc.tile * full, sc.tile * full)
                                : rounds * sc.tile + (rounds - 2.0f * floorf(0.5f * rounds)) * (sc.tile_alone - sc.tile);
     float cost = longest / S * work + rounds * sc.start + (lane > 0 ? sc.meet + sc.join * S : 0.0f);
-    if (lane > 0 && (n * S > (float)sc.groups || S > longest)) cost = INFINITY;
+    if (lane > 0 && (pieces > (float)sc.groups || S > longest)) cost = INFINITY;
     const float best = -total_of(-cost, -INFINITY, larger);
     const int at = __ffsll(__ballot(cost == best)) - 1;
     const float s_best = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(S), at));
@@ -455,9 +457,9 @@ struct PagedCursor {
   SeqBlock block;
   int at, end;
 };
-template <int BM, bool kStay> __device__ __forceinline__ PagedCursor first_item(const PagedAttnArgs& a, const PagedSchedule& sc) {
+template <int BM, bool kStay, bool kRagged = false> __device__ __forceinline__ PagedCursor first_item(const PagedAttnArgs& a, const PagedSchedule& sc) {
   PagedCursor c;
-  c.work = find_work<BM, kStay>(a, sc, c.block);
+  c.work = find_work<BM, kStay, kRagged>(a, sc, c.block);
   const int id = (int)blockIdx.x;
   if (!kStay) {   // (the grid is a multiple of eight, and has at least as many workgroups as there are pieces)
     const int per = (c.work.each * a.heads_kv + 7) / 8;
