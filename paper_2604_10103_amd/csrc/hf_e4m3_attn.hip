@@ -83,6 +83,8 @@ __device__ __forceinline__ uint32_t and_mask(float x, uint32_t mask, int k) {   
   return __float_as_uint(x) & (uint32_t)__builtin_amdgcn_sbfe((int)mask, k, 1);
 }
 
+constexpr int kNoKeys = 0x60000000;   // where a tile that there is not would start: behind every sequence (2^30), and no sum with it overflows
+
 // where the keys of an item's tiles lie: the pool's row (0 where there is none: read, and masked).  The wavefront keeps 64 entries of the
 // table, from ids_base on, a lane each.  Tiles start at multiples of 32
 struct PoolRows {
@@ -149,7 +151,7 @@ struct FullTiles {
 };
 
 // NaN codes next to rows that do not see them were left out: they enter the sums of the rows that do.  Off the fast path, key by key, straight
-// from the pages; add(codes of four features from `feature` on, in row `pool row`) for each key that exists
+// from the pages: add(key, the pool's row) for each key that exists, of the tiles that some row sees in part
 template <class Start, class Full, class F>
 __device__ __forceinline__ void each_key(const PagedAttnArgs& a, const PagedItem& it, const PoolRows& rows, int count, Start start_of, Full full, F add) {
 #pragma unroll 1
@@ -228,7 +230,7 @@ __global__ __launch_bounds__(64 * KS, sizeof(T) == 2 ? 2 : 1) void e4m3_few_kern
 
   // ---- the wavefront's tiles
   const int run = (it.t1 - it.t0 + KS - 1) / KS, base_tile = it.t0 + grp * run, count = max(0, min(run, it.t1 - base_tile));
-  const auto start_of = [&](int i) { return i < count ? kKeyTile * it.keys.tile(base_tile + i) : 0x7fffffe0; };
+  const auto start_of = [&](int i) { return i < count ? kKeyTile * it.keys.tile(base_tile + i) : kNoKeys; };
   const FullTiles full(a, it, base_tile, row_view(a, it, div_group(a, it.first)), row_view(a, it, div_group(a, x_last)), bad_pages);
 
   // ---- requests: a tile's 1 KB pieces, lane's row of piece j: RPP j + lane / UPR; and its scales, a lane each (K's, then V's)
@@ -496,7 +498,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void e4m3_chunk_ke
   }
   const bool bad_pages = any_bad_page(a, it);
   const int count = max(0, it.t1 - it.t0);
-  const auto start_of = [&](int i) { return i < count ? kKeyTile * it.keys.tile(it.t0 + i) : 0x7fffffe0; };
+  const auto start_of = [&](int i) { return i < count ? kKeyTile * it.keys.tile(it.t0 + i) : kNoKeys; };
   const FullTiles full(a, it, it.t0, row_view(a, it, div_group(a, min(it.first + 32 * wave, x_last))),
                        row_view(a, it, div_group(a, min(it.first + 32 * wave + 31, x_last))), bad_pages);
 

@@ -38,13 +38,66 @@ def test_attention(dtype, d, mask, batch, heads, heads_kv, page):
     ([1] * 70, [1 + i for i in range(70)], 40, 40, 64, 5, {}), ([300], [2100], 4, 1, 128, 64, {}), ([260, 130], [900, 130], 12, 12, 128, 100, {}),
     ([513], [1500], 8, 8, 64, 256, dict(causal=False)), ([700], [1400], 3, 3, 128, 350, dict(causal=False, window=700, n_sink=350)),
     ([1], [20000], 1, 1, 128, 16, dict(window=9000, n_sink=70)), ([1], [4000], 16, 1, 128, 4000, {}), ([1], [4000], 32, 1, 64, 1, {}),
-    ([3], [3000], 24, 2, 128, 48, dict(gain=6.0)), ([200], [600], 4, 2, 128, 48, dict(gain=6.0))])
+    ([3], [3000], 24, 2, 128, 48, dict(gain=6.0)), ([200], [600], 4, 2, 128, 48, dict(gain=6.0)),
+    # 16 and 32 rows by eight wavefronts, four, and one
+    ([1] * 90, [7 * i + 1 for i in range(90)], 8, 8, 128, 16, {}), ([6] * 10, [300 * i + 6 for i in range(10)], 8, 2, 128, 64, {}),
+    ([6] * 70, [6 + 5 * i for i in range(70)], 32, 8, 64, 16, {}), ([5] * 330, [5 + i % 60 for i in range(330)], 16, 4, 128, 16, {})])
 def test_longer(dtype, new, lens, heads, heads_kv, d, page, kw):
     b = Batch8(new, lens, heads, heads_kv, d, dtype, page, seed=len(lens) + d, **kw)
     O, lse2 = b.attend()
     b.check(O, lse2)
     again, _ = b.attend()
     assert torch.equal(O, again)
+
+
+def _reference(b):
+    """The oracle's answer by 64-bit products on the GPU, for many rows."""
+    n, d, group = b.n, b.d, b.heads // b.heads_kv
+    R, spread = np.full((n, b.heads, d), np.nan), np.full((n, b.heads, d), np.nan)
+    L, size, count = np.full((b.heads, n), np.nan), np.zeros((n, b.heads)), np.zeros(n, dtype=int)
+    K, V = (c.float().double() * s.double()[..., None] for c, s in ((b.K_pages, b.K_scales), (b.V_pages, b.V_scales)))
+    for s in range(len(b.lens)):
+        m, length, rows = int(b.cu[s + 1] - b.cu[s]), int(b.lens[s]), slice(int(b.cu[s]), int(b.cu[s + 1]))
+        pages = torch.tensor(b.table[s, :-(-length // b.page)], dtype=torch.long, device=DEV)
+        p, j = torch.arange(length - m, length, device=DEV)[:, None], torch.arange(length, device=DEV)[None]
+        sees = j <= p if b.mask["causal"] else j >= 0
+        if b.mask["window"]:
+            sees = sees & ((j > p - b.mask["window"]) | (j < b.mask["n_sink"]))
+        sees = sees.expand(m, length)
+        count[rows] = sees.sum(1).cpu().numpy()
+        for h in range(b.heads):
+            k, v = (x[pages, h // group].flatten(0, 1)[:length].contiguous() for x in (K, V))
+            q = b.Q[rows, h].double()
+            logit = (q @ k.T.contiguous() / d ** 0.5).masked_fill(~sees, -float("inf"))
+            w = torch.softmax(logit, -1)
+            R[rows, h], spread[rows, h] = f64(w @ v), f64(w @ v.abs())
+            L[h, rows] = f64(torch.logsumexp(logit, -1)) / np.log(2.0)
+            size[rows, h] = f64((q.abs() @ k.abs().T.contiguous() / d ** 0.5 * sees).amax(-1))
+    return R, L, spread, size, count
+
+
+@pytest.mark.parametrize("mask", [dict(causal=True), dict(causal=False, window=300, n_sink=70)])
+@pytest.mark.parametrize("new,lens,heads,heads_kv,page", [([600], [703], 64, 64, 50), ([513, 700], [513, 1500], 48, 24, 256), ([300], [2000], 64, 8, 16)])
+def test_256_rows_a_workgroup(mask, new, lens, heads, heads_kv, page):
+    b = Batch8(new, lens, heads, heads_kv, 128, "bf16", page, rows_behind=2, seed=page, **mask)
+    O, lse2 = b.attend()
+    b.check(O, lse2, _reference(b))
+    free = np.ones((b.n_pages, page), dtype=bool)              # what lies behind the sequences, in their pages and in others
+    for s, n in enumerate(lens):
+        for j in range(n):
+            free[b.table[s, j // page], j % page] = False
+    free = torch.tensor(free, device=DEV)[:, None].expand(b.K_scales.shape)
+    for codes, scales, x in ((b.K_pages, b.K_scales, float("inf")), (b.V_pages, b.V_scales, float("nan"))):
+        codes.view(torch.uint8)[free] = 0x7f
+        scales[free] = x
+    again, lse_again = b.attend()
+    assert torch.equal(O, again) and torch.equal(lse2, lse_again)
+
+
+def test_the_reference_is_the_oracle():
+    b = Batch8([5, 30], [90, 61], 6, 2, 64, "f32", 16, seed=1, causal=True, window=20, n_sink=3)
+    for x, y in zip(_reference(b), b.oracle()):
+        np.testing.assert_allclose(x, y, rtol=1e-9, atol=1e-12)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -223,3 +276,19 @@ def test_a_layer_of_serving():
         torch.cuda.synchronize()
         check(q, O, [1] * S)
     assert f64(scales[0]).min() >= 0
+
+
+def test_two_calls_at_once():
+    """Two streams, a workspace each; and a stream other than the tensors' own."""
+    bs = [Batch8([1] * 4, [3000, 50, 900, 2100], 8, 2, 128, "bf16", 16, seed=21), Batch8([60, 2], [900, 700], 8, 2, 128, "bf16", 16, seed=22)]
+    want = [b.attend(lse=False)[0] for b in bs]
+    streams = [torch.cuda.Stream() for _ in bs]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(3):
+        for b, stream in zip(bs, streams):
+            with torch.cuda.stream(stream):
+                got.append(b.attend(lse=False)[0])
+    torch.cuda.synchronize()
+    for k, O in enumerate(got):
+        assert torch.equal(O, want[k % 2])
