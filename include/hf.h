@@ -743,9 +743,10 @@ HF_API int hf_paged_e4m3_workspace_bytes(const hf_paged* cache, int32_t n_q, siz
 
 /* hf_paged_attn_fwd over pages in 8 bits: the same rows, masks, lse2, workspace rules and refusals.  Codes are multiplied as they are, a
  * key's scale with its score and a value's with its probability, so that nothing of the cache is rounded again: fp32 scores, statistics
- * and sums; in bf16 the product of probability and scale is rounded to bf16 for the second product.  What a token does not see, it does
- * not depend on, codes and scales that are NaN or infinite included; a NaN that it sees (code or scale) makes the outputs that it enters
- * NaN.  (Scales are meant as hf_paged_append_e4m3 writes them: what an infinite one that is seen gives is not defined.) */
+ * and sums.  In bf16 the product of probability and scale keeps 16 bits for the second product where a sequence has few rows on the average
+ * (n_q * heads / heads_kv <= 32 n_seqs), in chunks it is rounded to bf16.  What a token does not see, it does not depend on, codes and
+ * scales that are NaN or infinite included; a NaN that it sees (code or scale) makes the outputs that it enters NaN.  (Scales are meant as
+ * hf_paged_append_e4m3 writes them: what an infinite one that is seen gives is not defined.) */
 HF_API int hf_paged_attn_e4m3_fwd(const hf_paged* cache, const void* Q, const int64_t* q_strides, int32_t n_q,
                   const int32_t* cu_new, const int32_t* seq_lens, const void* K_pages, const void* V_pages, const float* K_scales,
                   const float* V_scales, const int32_t* page_table, void* O, const int64_t* o_strides, float* lse2_or_null,

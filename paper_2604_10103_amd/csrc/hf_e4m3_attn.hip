@@ -4,7 +4,10 @@
 // and multiplied on the bf16 matrix cores as they are.  A key's scale is a factor of its scores, a value's of its probability:
 //     s_j = c ks_j (q . kc_j),   o = sum_j (p_j vs_j) vc_j / sum_j p_j,
 // both in fp32.  fp32 queries and the products p vs are split into three bf16 each (8 + 8 + 8 bits: nothing is lost), whose products
-// accumulate in fp32; in bf16 the products p vs are rounded to bf16 once (half a step of each, which averages out over the keys).
+// accumulate in fp32.  In bf16 the products p vs are two bf16 where rows are few: 16 bits, and outputs as far off 64 bits as exact products
+// leave them, 1.66e-3, their own rounding (rounded to one bf16 2.34e-3).  That kernel waits for memory: 64 single tokens over 410 to 8191 keys
+// take 116.7 us, with one 115.8; 16 drafts of 8 tokens 48.9 and 48.2.  In chunks they are rounded to one (half a step of each, which averages
+// out over the keys: 2.3e-3), as there the second half costs a third: 12 heads x 4680 over 9360 to 14040 keys 624 us, with one 468.
 //
 // Both products are transposed, S^T = K Q^T and O^T += V^T P^T, so that a lane holds scores of one row and the exponentials are the second
 // product's operand as they lie.  Rows, work, parts and the end of an item are those of the other paged kernels (hf_paged_attn.h).
@@ -190,6 +193,7 @@ template <typename T, int D, int RB, int KS>
 __global__ __launch_bounds__(64 * KS, sizeof(T) == 2 ? 2 : 1) void e4m3_few_kernel(const E4m3Launch args) {
   using S = FewShape<D, RB, KS>;
   constexpr int BM = S::BM, TILE = S::TILE, SLOT = S::SLOT, PL = sizeof(T) == 2 ? 1 : 3;
+  constexpr int PP = sizeof(T) == 2 ? 2 : 3;               // bf16 of a product p vs (PL: of a query's element)
   constexpr int NS = D / 32, ND = D / 16;                  // steps of S^T, blocks of 16 features of O^T
   constexpr int RPP = 1024 / D, UPR = D / 16, NP = kKeyTile / RPP;   // rows of a 1 KB piece, 16-byte units of a row, pieces of a tile
   constexpr int REQ = 2 * NP + 1;                          // requests of a tile
@@ -348,7 +352,7 @@ __global__ __launch_bounds__(64 * KS, sizeof(T) == 2 ? 2 : 1) void e4m3_few_kern
           for (int e = 0; e < 2; ++e) vr[dt][e] = (int)((uint32_t)vr[dt][e] & ~((nan_codes((uint32_t)vr[dt][e]) >> 7) * 255u));
       }
     }
-    bf16x8 pf[RB][PL];
+    bf16x8 pf[RB][PP];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       float x[8];
@@ -396,10 +400,10 @@ __global__ __launch_bounds__(64 * KS, sizeof(T) == 2 ? 2 : 1) void e4m3_few_kern
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        __bf16 p[PL];
+        __bf16 p[PP];
         split(x[e], p);
 #pragma unroll
-        for (int pl = 0; pl < PL; ++pl) pf[rb][pl][e] = p[pl];
+        for (int pl = 0; pl < PP; ++pl) pf[rb][pl][e] = p[pl];
       }
     }
     // ---- O^T += V^T P^T
@@ -409,7 +413,7 @@ __global__ __launch_bounds__(64 * KS, sizeof(T) == 2 ? 2 : 1) void e4m3_few_kern
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
-        for (int pl = PL - 1; pl >= 0; --pl) o[rb][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[rb][pl], o[rb][dt], 0, 0, 0);
+        for (int pl = PP - 1; pl >= 0; --pl) o[rb][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[rb][pl], o[rb][dt], 0, 0, 0);
     }
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing may land on the sums
