@@ -683,7 +683,8 @@ typedef struct hf_paged {
 /* New keys, rotated by their positions, and new values enter the pages; the queries of the same tokens are rotated in the same launch.
  *   K_new, V_new  packed [n_new, heads_kv, head_dim]; Q, Q_out packed [n_new, heads, head_dim], both or neither; Q_out may be Q (same
  *             address and strides), otherwise their address ranges must be disjoint, and Q_out's rows may not overlap each other.
- *             K_new, V_new may interleave with Q_out (rows of one joint projection) but not share elements with it
+ *             K_new, V_new may interleave with Q_out (rows of one joint projection) but not share elements with it (refused where strides
+ *             and addresses leave it open)
  *   rope      NULL: keys (and queries) are copied as they are
  *   positions device int32 [n_axes, n_new]; NULL: a token's position on every axis is its place
  * A key is written as hf_rope_axes_apply would write it.  Two tokens of one call that name the same slot (tables that share a page
@@ -730,7 +731,8 @@ HF_API int hf_paged_attn_fwd(const hf_paged* cache, const void* Q, const int64_t
  *   rope, scaling, positions, K_new, V_new, Q, Q_out, n_new   as for hf_paged_append and hf_norm_rope_fwd; values are only quantised.
  *             Neither norm nor rope: keys are only quantised, queries copied
  * Two tokens of one call that name the same slot leave either of them there, or parts of both (codes of one, the scale of the other).
- * What is written (pages, scales, Q_out) lies over nothing else that the call is given. */
+ * What is written (pages, scales, Q_out) lies over nothing else that the call is given, but that Q_out may be Q and may interleave with
+ * K_new and V_new as for hf_paged_append. */
 HF_API int hf_paged_append_e4m3(const hf_paged* cache, const hf_head_norm* norm_or_null, const hf_rope_axes* rope_or_null,
                   const hf_rope_scaling* scaling_or_null, int32_t n_new, const void* K_new, const int64_t* k_strides, const void* V_new,
                   const int64_t* v_strides, const void* Q_or_null, const int64_t* q_strides, const float* k_weight_or_null,

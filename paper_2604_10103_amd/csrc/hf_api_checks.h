@@ -3,6 +3,8 @@
 
 #include <math.h>
 
+#include <numeric>
+
 #include "hf_common.h"
 
 namespace hf {
@@ -114,6 +116,39 @@ inline int check_apart(const View& x, const View& y, const char* what, bool in_p
 inline bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
   const char *x = static_cast<const char*>(a), *y = static_cast<const char*>(b);
   return x < y + nb && y < x + na;
+}
+
+// Whether x and y can be shown to have no byte in common though their rows may interleave (rows of one joint projection): for some period T,
+// what x covers of the places modulo T, an interval that its strides which T divides do not widen, lies beside what y covers.  Candidates are
+// their strides and the strides' common divisors
+inline bool interleave(const View& x, const View& y) {
+  if (!overlap(x.p, x.span(), y.p, y.span())) return true;
+  const auto beside = [&](int64_t T) {
+    const auto width = [&](const View& v) {
+      int64_t w = v.row * v.es;
+      for (int i = 0; i < v.dims; ++i)
+        if (v.stride[i] * v.es % T != 0) w += (v.n[i] - 1) * v.stride[i] * v.es;
+      return w;
+    };
+    const int64_t wx = width(x), wy = width(y), d = ((y.p - x.p) % T + T) % T;   // (x at 0, y at d)
+    return d >= wx && d + wy <= T;
+  };
+  const auto period = [](const View& v, int i) { return v.n[i] > 1 ? v.stride[i] * v.es : 0; };
+  for (int i = 0; i < x.dims; ++i)
+    if (period(x, i) > 0 && beside(period(x, i))) return true;
+  for (int j = 0; j < y.dims; ++j) {
+    if (period(y, j) > 0 && beside(period(y, j))) return true;
+    for (int i = 0; i < x.dims; ++i)
+      if (period(x, i) > 0 && period(y, j) > 0 && beside(std::gcd(period(x, i), period(y, j)))) return true;
+  }
+  return false;
+}
+
+// queries that are written while other workgroups read the new keys and values
+inline int check_queries_apart(const View& q_out, const View& k, const View& v) {
+  for (const View* x : {&k, &v})
+    if (!interleave(q_out, *x)) { set_error("Q_out overlaps %s", x == &k ? "K_new" : "V_new"); return HF_ERR_SHAPE; }
+  return HF_OK;
 }
 
 // What the call writes must not lie over what its later workgroups read

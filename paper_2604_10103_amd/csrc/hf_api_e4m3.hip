@@ -212,8 +212,8 @@ int hf_paged_append_e4m3(const hf_paged* cache, const hf_head_norm* norm_or_null
                        {k_weight_or_null, w * (each ? cache->heads_kv : 1), "k_weight"}, {q_weight_or_null, w * (each ? cache->heads : 1), "q_weight"},
                        span_of(q, "Q")};
   HF_TRY(check_written(written, 4, read, 9));
-  // (rows of one joint projection interleave: K_new and V_new may lie between the rows of Q_out)
   HF_TRY(check_written(written + 4, 1, read + 2, 6));
+  if (o.p) HF_TRY(check_queries_apart(o, k, v));
   for (int i = 0; i < 4; ++i)
     if (o.p && overlap(o.p, o.span(), written[i].p, written[i].bytes)) { set_error("Q_out overlaps %s", written[i].name); return HF_ERR_SHAPE; }
   return launch_append_e4m3(*cache, norm_or_null, rope_or_null, scaling_or_null, n_new, K_new, k.stride, V_new, v.stride, Q_or_null, q.stride,

@@ -77,6 +77,7 @@ int hf_paged_append(const hf_paged* cache, const hf_rope_axes* rope_or_null, int
     HF_TRY(check_packed(q, Q_or_null, "Q", q_strides, false));
     HF_TRY(check_packed(o, Q_out, "Q_out", q_out_strides, true));
     HF_TRY(check_apart(q, o, "Q_out overlaps Q without being Q", true));
+    HF_TRY(check_queries_apart(o, k, v));
     for (const View* x : {&q, &o})
       if (overlap(x->p, x->span(), K_pages, pool) || overlap(x->p, x->span(), V_pages, pool)) {
         set_error("%s overlaps the pages", x == &q ? "Q" : "Q_out");
