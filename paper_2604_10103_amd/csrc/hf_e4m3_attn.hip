@@ -835,7 +835,7 @@ Plan plan_of(const hf_paged& c, int n_q) {
     // 2000 119 and 105; and, where there is one for all 2048 wavefronts, a row tile a wavefront.
     if (tiles(p.rows) >= 2048) {
       p.ks = 1;
-      p.sc.groups = 2048;
+      p.sc.groups = kMostGroups;
       p.sc.tile = wide ? 3.2f : 1.6f;
       p.sc.tile_alone = wide ? 1.2f : 0.9f;
       p.sc.lead = 2;
@@ -879,9 +879,6 @@ Plan plan_of(const hf_paged& c, int n_q) {
   p.sc.meets = key_tiles > 1;
   return p;
 }
-
-// The counters' part of every workspace is as large, whatever the call: what a call of another shape left there are counters of its tag
-constexpr size_t kCounterBytes = 2 * 2048 * 8;
 
 template <auto* Kernel, class S> int launch(const E4m3Launch& l, int grid, hipStream_t s) {
   static LdsGrant grant;

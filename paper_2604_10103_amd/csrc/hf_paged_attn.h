@@ -63,6 +63,10 @@ struct PagedSchedule {
   unsigned long long tag;
 };
 
+// The counters' part of every workspace is as large, whatever the call and the pages' type: what another call left there are counters of its tag
+constexpr int kMostGroups = 2048;   // of a schedule
+constexpr size_t kCounterBytes = 2 * kMostGroups * 8;
+
 struct PagedLaunch {   // the kernels' only argument
   PagedAttnArgs a;
   PagedSchedule sc;

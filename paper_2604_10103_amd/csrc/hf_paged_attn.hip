@@ -513,9 +513,6 @@ Plan plan_of(const hf_paged& c, int n_q) {
   return p;
 }
 
-// The counters' part of every workspace is as large, whatever the call: what a call of another shape left there are counters of its tag
-constexpr size_t kCounterBytes = 2 * 1024 * 8;
-
 template <int D, int NW, int KS, bool kBig> int launch(const PagedAttnArgs& a, const PagedSchedule& sc, int grid, hipStream_t s) {
   using S = Shape<D, NW, KS>;
   static LdsGrant grant;
