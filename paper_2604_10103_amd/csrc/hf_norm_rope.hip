@@ -340,24 +340,25 @@ struct AppendArgs {
 };
 
 // x[] as e4m3 with the row's scale: the quotients are rounded as a division is, which decides where one lies half way between two codes, then
-// to a code.  A product with the rounded reciprocal is off by 1.5 units at most, and one correction by its remainder rounds it correctly, but
-// for a divisor whose mantissa is all ones (7 2^k over 448 is one): its reciprocal is taken rounded up.  (Markstein's theorem; three
-// instructions a quotient where a division takes ten.)
+// to a code.  A product with the rounded reciprocal is off by 1.5 units at most, and one correction by its remainder rounds it correctly
+// (Markstein's theorem; three instructions a quotient where a division takes ten), as long as the remainder is exact: below a scale of 2^-93 its
+// last bits are beyond fp32 where the quotient is 2^-10, the least that decides about a code, and row and scale are taken 2^64 times as large.
+// (The theorem spares one divisor, an all-ones mantissa.  The product with 1 / 448 has it for no row.)
 template <int N, int TPR> __device__ __forceinline__ float quantise(const float (&x)[N], uint32_t (&c)[N / 4]) {
   uint32_t top = 0;
 #pragma unroll
   for (int e = 0; e < N; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);   // (as integers: a NaN is larger than all others)
   top = max_over_row<TPR>(top);
   const bool finite = top < 0x7f800000u;
-  const float scale = fmaxf(__uint_as_float(top) * (1.0f / 448.0f), 0x1p-126f), rounded = 1.0f / scale;
-  const float inv = (__float_as_uint(scale) & 0x7fffffu) == 0x7fffffu ? __uint_as_float(__float_as_uint(rounded) + 1) : rounded;
+  const float scale = fmaxf(__uint_as_float(top) * (1.0f / 448.0f), 0x1p-126f);
+  const float up = scale < 0x1p-90f ? 0x1p64f : 1.0f, by = scale * up, inv = 1.0f / by;
 #pragma unroll
   for (int e = 0; e < N; e += 4) {
     float q[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float y = x[e + i] * inv;
-      q[i] = copysignf(fmaf(fmaf(-y, scale, x[e + i]), inv, y), x[e + i]);   // (a zero keeps its sign)
+      const float v = x[e + i] * up, y = v * inv;
+      q[i] = copysignf(fmaf(fmaf(-y, by, v), inv, y), v);   // (a zero keeps its sign)
     }
     uint32_t w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
     w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], (int)w, true);
