@@ -622,8 +622,8 @@ typedef struct hf_rope_scaling {
  *   scaling    NULL: none
  *   X, Y, their strides, positions, n_tokens   as for hf_rope_axes_apply: strided rows, Y may be X, 0 tokens
  *   weight     device fp32 as norm->per_head says, contiguous, NULL: ones; not over Y
- * fp32 arithmetic with one rounding to dtype; squares are summed in fp32 (a row of values beyond 2^60 or of an infinity has no finite
- * norm, a row of zeros with eps = 0 becomes NaN). */
+ * fp32 arithmetic with one rounding to dtype; squares are summed in fp32, of rows whose squares would leave it times a power of two (rows
+ * of any size have their norm; an infinity has none, and a row of zeros with eps = 0 becomes NaN). */
 HF_API int hf_norm_rope_fwd(const hf_head_norm* norm_or_null, const hf_rope_axes* rope_or_null, const hf_rope_scaling* scaling_or_null,
                   int32_t dtype, int32_t head_dim, int32_t batch, int32_t heads, int32_t n_tokens, const void* X, const int64_t* x_strides,
                   const float* weight_or_null, const int32_t* positions, int32_t positions_per_batch, void* Y, const int64_t* y_strides,

@@ -133,12 +133,27 @@ template <typename T, int D, int MODE> struct Part {
       x[b] = turns ? v : x[b];
     }
   }
-  // 1 / sqrt(mean square + eps)
+  // r = 1 / sqrt(mean square + eps).  Where the squares leave fp32, of the row times a power of two: a large row's r is brought back (down to
+  // 2^-128, where it has 22 bits); a small one's might be too large itself, and -r' stands for it, of the row times kLarger
+  static constexpr float kLarger = 0x1p100f, kSmaller = 0x1p-72f;
   __device__ static __forceinline__ float inverse_rms(const float (&x)[NF], float eps) {
-    float s = 0.0f;
+    const auto mean = [&](float by, float more) {
+      float s = 0.0f;
 #pragma unroll
-    for (int i = 0; i < NF; ++i) s = fmaf(x[i], x[i], s);
-    return rsqrtf(sum_over_row<TPR>(s) * (1.0f / D) + eps);
+      for (int i = 0; i < NF; ++i) s = fmaf(x[i] * by, x[i] * by, s);
+      return sum_over_row<TPR>(s) * (1.0f / D) + more;
+    };
+    const float m = mean(1.0f, eps);
+    if (m < 0x1p-100f) return -rsqrtf(mean(kLarger, eps * kLarger * kLarger));   // (a row's threads go the same way)
+    if (m > 0x1p100f) return rsqrtf(mean(kSmaller, eps * kSmaller * kSmaller)) * kSmaller;
+    return rsqrtf(m);
+  }
+  // x as r is meant for it
+  __device__ static __forceinline__ void fit(float r, float (&x)[NF]) {
+    if (r < 0.0f) {
+#pragma unroll
+      for (int i = 0; i < NF; ++i) x[i] *= -kLarger;
+    }
   }
 };
 
@@ -174,6 +189,7 @@ __device__ __forceinline__ void norm_rows(const NormArgs& n, const Angles<D, MOD
       float x[NF];
       R::widen(raw[u], x);
       if (!shared) R::weights(weight(i + u), g, P, w);
+      R::fit(r[u], x);
 #pragma unroll
       for (int e = 0; e < NF; ++e) x[e] = x[e] * r[u] * w[e];
       R::turn(t, g, P, x);
@@ -274,8 +290,9 @@ __global__ __launch_bounds__(256) void norm_rope_bwd_kernel(const AxesSpec spec,
         R::widen(rg[u], y);
         R::turn(t, g, P, y);
         if (a.norm.on) {
-          const float r = R::inverse_rms(v, a.norm.eps);
           if (!shared) R::weights(a.weight + (long long)(h + u) * D, g, P, w);
+          const float r = R::inverse_rms(v, a.norm.eps);
+          R::fit(r, v);
           float dot = 0.0f;
 #pragma unroll
           for (int e = 0; e < NF; ++e) {
@@ -287,6 +304,7 @@ __global__ __launch_bounds__(256) void norm_rope_bwd_kernel(const AxesSpec spec,
           dot = sum_over_row<TPT>(dot) * (1.0f / D);
 #pragma unroll
           for (int e = 0; e < NF; ++e) y[e] = r * (y[e] - v[e] * dot);
+          R::fit(r, y);
         }
         R::store(dx + (h + u) * a.dh, g, P, y);
       }
