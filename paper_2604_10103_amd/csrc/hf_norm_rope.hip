@@ -10,6 +10,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "hf_e4m3.h"
 #include "hf_rope_axes.h"
@@ -238,8 +239,9 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(const AxesSpec spec, con
 
 // ---- gradients.  With g the output's gradient turned back and u the row at unit mean square,
 //     dX = r (w g - u mean(w g u)),  dweight = sum g u:
-// one pass over X and dY.  Every thread sums its features of dweight over all its rows, in fp32; a workgroup's threads meet in LDS, and the
-// workgroups' sums lie in the workspace until a second launch adds them, in a fixed order, both in 64 bits
+// one pass over X and dY.  Every thread sums its features of dweight over 16 of its rows at a time in fp32, and those sums in 64 bits in LDS
+// (600 equal rows summed in fp32 alone are off by up to 146 units of 2^-24, 16 by 16 at most); a workgroup's threads meet there, and the workgroups' sums,
+// rounded to fp32, lie in the workspace until a second launch adds them in 64 bits.  All in a fixed order
 struct BwdArgs {
   const void *X, *dY;
   void* dX;
@@ -252,16 +254,24 @@ struct BwdArgs {
   NormArgs norm;
 };
 
-template <typename T, int D, int MODE>
+constexpr int kChain = 16;
+
+template <typename T, int D, int MODE, bool CHAINS>   // CHAINS: a thread may have more than kChain rows
 __global__ __launch_bounds__(256) void norm_rope_bwd_kernel(const AxesSpec spec, const BwdArgs a) {
   typedef Part<T, D, MODE> R;
   constexpr int TPT = R::TPR, TOK = 256 / TPT, NF = R::NF, U = 1;
   const int g = threadIdx.x % TPT, P = spec.pairs;
   const int per = (a.heads + gridDim.y - 1) / gridDim.y, h0 = blockIdx.y * per, h1 = min(a.heads, h0 + per);
   const bool shared = !a.norm.per_head || !a.weight;
+  __shared__ std::conditional_t<CHAINS, double, float> sums[256 * NF];   // chains' [NF][thread]; in the end [TOK][D]
   float w[NF], dw[NF];
+  int chain = 0;   // rows in dw
 #pragma unroll
   for (int e = 0; e < NF; ++e) dw[e] = 0.0f;
+  if constexpr (CHAINS) {
+#pragma unroll
+    for (int e = 0; e < NF; ++e) sums[256 * e + threadIdx.x] = 0.0;
+  }
   if (shared) R::weights(a.weight, g, P, w);
   for (int tok = blockIdx.x * TOK + threadIdx.x / TPT; tok < a.n; tok += gridDim.x * TOK) {
     const int32_t* pos = a.positions + blockIdx.z * a.pos_batch + tok;
@@ -307,18 +317,36 @@ __global__ __launch_bounds__(256) void norm_rope_bwd_kernel(const AxesSpec spec,
           R::fit(r, y);
         }
         R::store(dx + (h + u) * a.dh, g, P, y);
+        if constexpr (CHAINS) {
+          if (++chain == kChain) {
+            chain = 0;
+#pragma unroll
+            for (int e = 0; e < NF; ++e) {
+              sums[256 * e + threadIdx.x] += (double)dw[e];
+              dw[e] = 0.0f;
+            }
+          }
+        }
       }
     }
   }
   if (!a.partial) return;   // (uniform)
-  __shared__ float sums[TOK][D];
+  if constexpr (CHAINS) {
+    double mine[NF];
 #pragma unroll
-  for (int e = 0; e < NF; ++e) sums[threadIdx.x / TPT][R::feature(g, P, e)] = dw[e];
+    for (int e = 0; e < NF; ++e) mine[e] = sums[256 * e + threadIdx.x] + (double)dw[e];
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < NF; ++e) sums[threadIdx.x / TPT * D + R::feature(g, P, e)] = mine[e];
+  } else {
+#pragma unroll
+    for (int e = 0; e < NF; ++e) sums[threadIdx.x / TPT * D + R::feature(g, P, e)] = dw[e];
+  }
   __syncthreads();
   if (threadIdx.x < D) {
     double total = 0.0;   // (of either sign: sums in 32 bits would cost half a digit)
 #pragma unroll
-    for (int i = 0; i < TOK; ++i) total += (double)sums[i][threadIdx.x];
+    for (int i = 0; i < TOK; ++i) total += (double)sums[i * D + threadIdx.x];
     const float s = (float)total;
     const int row = a.norm.per_head ? blockIdx.y : 0, shares = a.norm.per_head ? 1 : gridDim.y, share = a.norm.per_head ? 0 : blockIdx.y;
     const int parts = gridDim.x * gridDim.z * shares, part = (blockIdx.z * shares + share) * gridDim.x + blockIdx.x;
@@ -571,13 +599,21 @@ int launch_norm_rope_bwd(const hf_head_norm* norm, const hf_rope_axes* r, const 
   const AxesMode mode = r ? axes_mode(*r, spec.pairs) : kAdjacent;
   const BwdGrid b = bwd_grid(D, mode == kAdjacent ? D / 8 : D / 16, batch, heads, n, norm && norm->per_head);
   if (n > 0) {
+    const int tok = mode == kAdjacent ? 2048 / D : 4096 / D;
+    const long long rows = ((long long)n + b.x * tok - 1) / (b.x * tok) * ((heads + b.y - 1) / b.y);   // of a thread
     const BwdArgs a = {X, dY, dX, weight, positions, dweight ? static_cast<float*>(workspace) : nullptr,
                        xs[0], xs[1], xs[2], gs[0], gs[1], gs[2], ds[0], ds[1], ds[2],
                        per_batch && r ? (long long)r->n_axes * n : 0, n, heads, norm_args(norm, sc)};
     const dim3 grid(b.x, b.y, b.z);
-#define HF_GO(T, DD, M) hipLaunchKernelGGL((norm_rope_bwd_kernel<T, DD, M>), grid, dim3(256), 0, s, spec, a)
-    HF_ROPE_TYPES(dtype, D, mode, HF_GO);
+    if (dweight && rows > kChain) {
+#define HF_GO(T, DD, M) hipLaunchKernelGGL((norm_rope_bwd_kernel<T, DD, M, true>), grid, dim3(256), 0, s, spec, a)
+      HF_ROPE_TYPES(dtype, D, mode, HF_GO);
 #undef HF_GO
+    } else {
+#define HF_GO(T, DD, M) hipLaunchKernelGGL((norm_rope_bwd_kernel<T, DD, M, false>), grid, dim3(256), 0, s, spec, a)
+      HF_ROPE_TYPES(dtype, D, mode, HF_GO);
+#undef HF_GO
+    }
     const int rc = check_launch("hf_norm_rope_bwd");
     if (rc != HF_OK) return rc;
   }
