@@ -134,26 +134,27 @@ template <typename T, int D, int MODE> struct Part {
       x[b] = turns ? v : x[b];
     }
   }
-  // r = 1 / sqrt(mean square + eps).  Where the squares leave fp32, of the row times a power of two: a large row's r is brought back (down to
-  // 2^-128, where it has 22 bits); a small one's might be too large itself, and -r' stands for it, of the row times kLarger
-  static constexpr float kLarger = 0x1p100f, kSmaller = 0x1p-72f;
-  __device__ static __forceinline__ float inverse_rms(const float (&x)[NF], float eps) {
-    const auto mean = [&](float by, float more) {
+  // r = 1 / sqrt(mean square + eps) of the row times k, which x[] is multiplied by: a power of two where the squares leave fp32, else 1
+  __device__ static __forceinline__ float inverse_rms(float (&x)[NF], float eps, float& k) {
+    const auto mean = [&](float more) {
       float s = 0.0f;
 #pragma unroll
-      for (int i = 0; i < NF; ++i) s = fmaf(x[i] * by, x[i] * by, s);
+      for (int i = 0; i < NF; ++i) s = fmaf(x[i], x[i], s);
       return sum_over_row<TPR>(s) * (1.0f / D) + more;
     };
-    const float m = mean(1.0f, eps);
-    if (m < 0x1p-100f) return -rsqrtf(mean(kLarger, eps * kLarger * kLarger));   // (a row's threads go the same way)
-    if (m > 0x1p100f) return rsqrtf(mean(kSmaller, eps * kSmaller * kSmaller)) * kSmaller;
+    k = 1.0f;
+    float m = mean(eps);
+    if (m < 0x1p-100f || m > 0x1p100f) {   // (a row's threads go the same way)
+      k = m < 1.0f ? 0x1p100f : 0x1p-72f;
+      times(k, x);
+      m = mean(eps * k * k);
+    }
     return rsqrtf(m);
   }
-  // x as r is meant for it
-  __device__ static __forceinline__ void fit(float r, float (&x)[NF]) {
-    if (r < 0.0f) {
+  __device__ static __forceinline__ void times(float k, float (&x)[NF]) {
+    if (k != 1.0f) {
 #pragma unroll
-      for (int i = 0; i < NF; ++i) x[i] *= -kLarger;
+      for (int i = 0; i < NF; ++i) x[i] *= k;
     }
   }
 };
@@ -177,12 +178,13 @@ __device__ __forceinline__ void norm_rows(const NormArgs& n, const Angles<D, MOD
     typename R::Raw raw[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) raw[u] = R::load(from(min(i + u, i1 - 1)), g, P);
-    float r[U];
+    float r[U], k[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       float x[NF];
       R::widen(raw[u], x);
-      r[u] = n.on ? R::inverse_rms(x, n.eps) : 1.0f;
+      r[u] = k[u] = 1.0f;
+      if (n.on) r[u] = R::inverse_rms(x, n.eps, k[u]);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -190,7 +192,7 @@ __device__ __forceinline__ void norm_rows(const NormArgs& n, const Angles<D, MOD
       float x[NF];
       R::widen(raw[u], x);
       if (!shared) R::weights(weight(i + u), g, P, w);
-      R::fit(r[u], x);
+      R::times(k[u], x);
 #pragma unroll
       for (int e = 0; e < NF; ++e) x[e] = x[e] * r[u] * w[e];
       R::turn(t, g, P, x);
@@ -301,8 +303,8 @@ __global__ __launch_bounds__(256) void norm_rope_bwd_kernel(const AxesSpec spec,
         R::turn(t, g, P, y);
         if (a.norm.on) {
           if (!shared) R::weights(a.weight + (long long)(h + u) * D, g, P, w);
-          const float r = R::inverse_rms(v, a.norm.eps);
-          R::fit(r, v);
+          float k;
+          const float r = R::inverse_rms(v, a.norm.eps, k);
           float dot = 0.0f;
 #pragma unroll
           for (int e = 0; e < NF; ++e) {
@@ -314,7 +316,7 @@ __global__ __launch_bounds__(256) void norm_rope_bwd_kernel(const AxesSpec spec,
           dot = sum_over_row<TPT>(dot) * (1.0f / D);
 #pragma unroll
           for (int e = 0; e < NF; ++e) y[e] = r * (y[e] - v[e] * dot);
-          R::fit(r, y);
+          R::times(k, y);
         }
         R::store(dx + (h + u) * a.dh, g, P, y);
         if constexpr (CHAINS) {

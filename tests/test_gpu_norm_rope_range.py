@@ -84,7 +84,7 @@ def test_a_power_of_two_changes_nothing(dtype, by):
 
 
 def test_the_largest_rows():
-    """Without rotation 15 of the bound's 21 units are spent; at 2^-128 r has 22 bits, which is four more."""
+    """Without a rotation 15 of the bound's 21 units are counted."""
     top = torch.finfo(torch.float32).max
     x = torch.tensor([1.0, -1.0, 0.5, 2.0 ** -60]).repeat(16).mul(top)[None, None].to(DEV)
     y = torch.empty_like(x)
