@@ -822,7 +822,9 @@ Plan plan_of(const hf_paged& c, int n_q) {
   if (p.rows == 128 && c.dtype == HF_BF16 && c.head_dim == 128 && rows > 128ll * c.n_seqs) {
     const long long n = (rows + c.n_seqs - 1) / c.n_seqs, heads = (long long)c.n_seqs * c.heads_kv;   // (as if all were as long)
     auto rounds = [&](int of) { return (double)(((n + of - 1) / of * heads + 255) / 256); };
-    if (rounds(256) * 1.10 <= rounds(128) * 0.595) p.rows = 256;   // (microseconds a tile: 12 heads x 4680 over 9360 to 14040 keys 482 and 522, measured together)
+    // (microseconds a tile when both were last measured together, 482 and 522 for 12 heads x 4680 over 9360 to 14040 keys; the schedule below has
+    // the later 0.89 and 0.535.  Starts are not counted: 8 x 512 over 1500 keys take 82 us by 256 rows, which the rule takes, and 72 by 128)
+    if (rounds(256) * 1.10 <= rounds(128) * 0.595) p.rows = 256;
   }
   p.ks = p.rows <= 32 ? 4 : 1;
   const bool wide = c.head_dim == 128;
@@ -856,7 +858,7 @@ Plan plan_of(const hf_paged& c, int n_q) {
     p.sc.meet = 5.0f;
     p.sc.join = 0.1f;
   } else {
-    p.sc.units = 256.0f;
+    p.sc.units = 256.0f;            // (two or three workgroups that run on a unit at a time share its products)
     p.sc.groups = 65536 / p.rows;   // (at most 512)
     p.sc.meet = 6.0f;
     p.sc.join = 1.0f;

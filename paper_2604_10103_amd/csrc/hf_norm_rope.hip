@@ -4,8 +4,8 @@
 // All move every row once: they are bound by memory.  A thread owns the same 8 or 16 features of a token for several heads, so that an angle
 // is formed once and serves them all; a row's 4 to 16 threads exchange their sums of squares (and the gradient's products, and the largest
 // magnitude of a row that is quantised) by data-parallel moves within 16 lanes, three or four instructions a sum.  Two rows are requested
-// before the first one is worked on.  10800 tokens of 40 rows pass in 47 us, 4.7 TB/s; the gradients of 9360 tokens of 12 rows take 21 us, 4.1 TB/s
-// and the launch that adds the weights' sums; 9360 tokens of 12 keys, values and queries enter the pages in 32 to 35 us, 4.1 to 4.5 TB/s, of which
+// before the first one is worked on.  10800 tokens of 40 rows pass in 47 us, 4.7 TB/s; the gradients of 9360 tokens of 12 rows take 21 to 22 us,
+// 3.9 to 4.1 TB/s and the launch that adds the weights' sums; 9360 tokens of 12 keys, values and queries enter the pages in 33 to 36 us, 4.0 to 4.4 TB/s, of which
 // some 4 are the launch and the chain lengths, page table, rows; a token of 40 rows takes 4 to 5 us, 64 single tokens are appended in 5.6.
 #include <math.h>
 
@@ -506,8 +506,9 @@ __global__ __launch_bounds__(256) void append_e4m3_kernel(const AxesSpec spec, c
 }
 
 // shares of a token's rows: at least 1024 workgroups, or as many as leave each four rows, which an angle formed once serves; but no more than
-// the `resident` ones that run at a time, whose registers let the compute units have so many: 10800 tokens of 40 rows 47.2 us by 2025
-// workgroups, 48.5 by 2700; 9360 tokens of 36 rows into the pages 30.2 by 1170, 34.7 by 2340
+// `resident` ones, which is how many run at a time in ADJACENT (56 and 74 registers: eight and six wavefronts a SIMD): 10800 tokens of 40 rows
+// 47.2 us by 2025 workgroups, 48.5 by 2700; 9360 tokens of 36 rows into the pages 30.2 by 1170, 34.7 by 2340.  HALVES has registers for 1024
+// (114 to 122), with any number of pairs for 512 or 768 (149 to 200); other bounds were not measured for these
 int shares(long long groups, int rows, int resident) {
   const long long s = std::min(std::max(1ll, resident / groups), std::max((1024 + groups - 1) / groups, (long long)rows / 4));
   return (int)std::max(1ll, std::min(s, (long long)rows));

@@ -25,3 +25,15 @@ def test_few_rows_round_bf16_outputs_once(d, new, lens, heads, heads_kv):
     bound = HALF["bf16"] * np.abs(R) + spread * (2.0 ** -16 + 2 * delta + 2 * sums)
     far = np.abs(f64(O) - R) - bound
     assert (far <= 0).all(), f"{(far > 0).mean():.3e} of the values beyond the bound, by {far.max():.3e}"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [[1, 2], [60, 3]])
+@pytest.mark.parametrize("size", [-100, 100])
+def test_values_of_the_sizes_that_keep_their_precision(dtype, new, size):
+    """Scales of values between 2^-100 and 2^100: parts of p v_scale below 2^-134 are lost, 2^-30 of a sum of such sizes and less than one of
+    the 64 roundings that the bound counts beside a sum's own; a sum of products of up to 2^8, 448 and 2^100 is finite."""
+    b = Batch8(new, [300, 70], 4, 2, 64, dtype, 16, seed=3)
+    top = float(b.V_scales.max())
+    b.V_scales.mul_(2.0 ** size / top).clamp_min_(2.0 ** -100)
+    b.check(*b.attend())
