@@ -13,7 +13,7 @@
 // product's operand as they lie.  Rows, work, parts and the end of an item are those of the other paged kernels (hf_paged_attn.h).
 //
 // Two kernels:
-//   few rows (16 or 32 a workgroup: single tokens)   bound by memory: 64 single tokens over 410 to 8191 keys 116 us, 5.2 TB/s.  Every wavefront
+//   few rows (16 or 32 a workgroup: single tokens)   bound by memory: 64 single tokens over 410 to 8191 keys 117 us, 5.1 TB/s.  Every wavefront
 //                                                    reads its own tiles as bytes, global -> LDS directly, and converts what it has read into registers
 //   chunks (128 or 256 rows a workgroup)             bound by the vector unit beside the matrix cores: 12 heads x 4680 over 9360 to 14040 keys
 //                                                    467 us, 800 TFLOP/s.  K is converted once on its way into LDS, where all wavefronts read it as bf16
@@ -822,8 +822,9 @@ Plan plan_of(const hf_paged& c, int n_q) {
   if (p.rows == 128 && c.dtype == HF_BF16 && c.head_dim == 128 && rows > 128ll * c.n_seqs) {
     const long long n = (rows + c.n_seqs - 1) / c.n_seqs, heads = (long long)c.n_seqs * c.heads_kv;   // (as if all were as long)
     auto rounds = [&](int of) { return (double)(((n + of - 1) / of * heads + 255) / 256); };
-    // (microseconds a tile when both were last measured together, 482 and 522 for 12 heads x 4680 over 9360 to 14040 keys; the schedule below has
-    // the later 0.89 and 0.535.  Starts are not counted: 8 x 512 over 1500 keys take 82 us by 256 rows, which the rule takes, and 72 by 128)
+    // (microseconds a tile of two earlier kernels; the schedule below has 0.89 and 0.535, a ratio of 1.66 for 1.85.  12 heads x 4680 over 9360 to
+    // 14040 keys take 470 us by 256 rows, 516 by 128; 16 heads x 8 x 512 over 2012 85 and 90.  Where lengths differ the rule, which does not know
+    // them, errs: 8 sequences of up to 512 new over up to 1500 take 82 by 256 rows, which it chooses, and 71 by 128)
     if (rounds(256) * 1.10 <= rounds(128) * 0.595) p.rows = 256;
   }
   p.ks = p.rows <= 32 ? 4 : 1;
