@@ -750,8 +750,8 @@ HF_API int hf_paged_e4m3_workspace_bytes(const hf_paged* cache, int32_t n_q, siz
  * scales that are NaN or infinite included; a NaN that it sees (code or scale) makes the outputs that it enters NaN.  (Scales are meant as
  * hf_paged_append_e4m3 writes them: what an infinite one that is seen gives is not defined.  Values keep their precision where their
  * scales are between 2^-100 and 2^100: what probability and scale make of a smaller one ends at 2^-134, sums of larger ones may leave fp32.)
- * Single tokens take half the time that they take over bf16 pages; chunks and prompts, bound by their products, take longer, a fifth to a
- * quarter, as codes are widened and scales applied on the way. */
+ * Single tokens over long contexts take half the time that they take over bf16 pages; chunks and prompts, bound by their products, take a
+ * fifth to a quarter longer, as codes are widened and scales applied on the way. */
 HF_API int hf_paged_attn_e4m3_fwd(const hf_paged* cache, const void* Q, const int64_t* q_strides, int32_t n_q,
                   const int32_t* cu_new, const int32_t* seq_lens, const void* K_pages, const void* V_pages, const float* K_scales,
                   const float* V_scales, const int32_t* page_table, void* O, const int64_t* o_strides, float* lse2_or_null,

@@ -5,8 +5,9 @@
 // is formed once and serves them all; a row's 4 to 16 threads exchange their sums of squares (and the gradient's products, and the largest
 // magnitude of a row that is quantised) by data-parallel moves within 16 lanes, three or four instructions a sum.  Two rows are requested
 // before the first one is worked on.  10800 tokens of 40 rows pass in 47 us, 4.7 TB/s; the gradients of 9360 tokens of 12 rows take 21 to 22 us,
-// 3.9 to 4.1 TB/s and the launch that adds the weights' sums; 9360 tokens of 12 keys, values and queries enter the pages in 33 to 36 us, 4.0 to 4.4 TB/s, of which
-// some 4 are the launch and the chain lengths, page table, rows; a token of 40 rows takes 4 to 5 us, 64 single tokens are appended in 5.6.
+// 3.9 to 4.1 TB/s and the launch that adds the weights' sums; 9360 tokens of 12 keys, values and queries enter the pages in 33 to 36 us, 4.0 to
+// 4.4 TB/s, of which some 4 are the launch and the chain lengths, page table, rows; a token of 40 rows takes 4 to 5 us, 64 single tokens are
+// appended in 5.9.
 #include <math.h>
 
 #include <algorithm>
@@ -136,18 +137,19 @@ template <typename T, int D, int MODE> struct Part {
   }
   // r = 1 / sqrt(mean square + eps) of the row times k, which x[] is multiplied by: a power of two where the squares leave fp32, else 1
   __device__ static __forceinline__ float inverse_rms(float (&x)[NF], float eps, float& k) {
-    const auto mean = [&](float more) {
+    const auto mean = [&] {
       float s = 0.0f;
 #pragma unroll
       for (int i = 0; i < NF; ++i) s = fmaf(x[i], x[i], s);
-      return sum_over_row<TPR>(s) * (1.0f / D) + more;
+      return sum_over_row<TPR>(s) * (1.0f / D);
     };
     k = 1.0f;
-    float m = mean(eps);
-    if (m < 0x1p-100f || m > 0x1p100f) {   // (a row's threads go the same way)
-      k = m < 1.0f ? 0x1p100f : 0x1p-72f;
+    const float square = mean();
+    float m = square + eps;
+    if (m < 0x1p-100f || square > 0x1p100f) {   // (a row's threads go the same way)
+      k = m < 0x1p-100f ? 0x1p100f : 0x1p-72f;
       times(k, x);
-      m = mean(eps * k * k);
+      m = mean() + eps * k * k;
     }
     return rsqrtf(m);
   }
@@ -242,8 +244,8 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(const AxesSpec spec, con
 // ---- gradients.  With g the output's gradient turned back and u the row at unit mean square,
 //     dX = r (w g - u mean(w g u)),  dweight = sum g u:
 // one pass over X and dY.  Every thread sums its features of dweight over 16 of its rows at a time in fp32, and those sums in 64 bits in LDS
-// (600 equal rows summed in fp32 alone are off by up to 146 units of 2^-24, 16 by 16 at most); a workgroup's threads meet there, and the workgroups' sums,
-// rounded to fp32, lie in the workspace until a second launch adds them in 64 bits.  All in a fixed order
+// (600 equal rows summed in fp32 alone are off by up to 146 units of 2^-24, 16 by 16 at most); a workgroup's threads meet there, and the
+// workgroups' sums, rounded to fp32, lie in the workspace until a second launch adds them in 64 bits.  All in a fixed order
 struct BwdArgs {
   const void *X, *dY;
   void* dX;

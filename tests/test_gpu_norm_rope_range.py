@@ -93,6 +93,16 @@ def test_the_largest_rows():
     assert (np.abs(f64(y) - want) <= 21 * UNIT * np.abs(want)).all()
 
 
+def test_rows_below_a_large_eps():
+    """An eps beyond 2^100 leaves small rows small: no bit is lost until the results are subnormal."""
+    x, _ = _rows("f32", 64, 3)
+    y = torch.empty_like(x)
+    for eps in (1e29, 1e33, 3e38):
+        hf.hf_norm_rope_fwd(x, y, norm=hf.make_head_norm(eps))
+        want = orc.norm(f64(x), float(np.float32(eps)))[0]
+        assert (np.abs(f64(y) - want) <= 21 * UNIT * np.abs(want) + 2.0 ** -149).all()
+
+
 def test_what_has_no_norm_has_none():
     x = torch.full((1, 1, 4, 64), 2.0 ** -80, device=DEV)
     x[0, 0, 1, 3], x[0, 0, 2, 3] = float("nan"), float("inf")
